@@ -69,6 +69,9 @@ extern "C" {
 /* ---- element types ----------------------------------------------------- */
 #define MALT_F32   0
 #define MALT_BF16  1
+/* index types (token ids, positions) */
+#define MALT_I32   2
+#define MALT_I64   3
 
 /* One 2-D parameter.  All pointers are DEVICE pointers owned by the caller,
  * 16-byte aligned, row-major and densely packed (leading dimension = cols).
@@ -426,6 +429,140 @@ int malt_adamw_set_step(malt_adamw_state_t* st, int64_t t_host);
 
 /* Free the state (synchronises with its last stream first). */
 void malt_adamw_destroy_state(malt_adamw_state_t* st);
+
+/* ---- Model operators -----------------------------------------------------
+ * The passes of a transformer's training step that make gradients for the
+ * tensors updated above and are not matrix products: the embedding lookup (its
+ * gradient goes to the token embedding, which may be tied with the output
+ * head), the norms of queries and keys with the position rotation (to the
+ * attention input matrix and two gain vectors) and distillation from a
+ * teacher's top logits (to the output head and everything below it).
+ *
+ * Every call is stateless and asynchronous on `stream`, works on the current
+ * device, allocates nothing and reads and writes only what it is given.
+ * Pointers need the alignment of their element type only (workspaces 16
+ * bytes); 16-byte aligned rows run faster.  Strides and leading dimensions
+ * count elements, and offsets are 64-bit.  Tensors are MALT_F32 or MALT_BF16
+ * as given per argument, all arithmetic is fp32 and each result is rounded
+ * once.  Results depend on the inputs and their alignment alone (no sum is
+ * ordered by timing).
+ * Outputs must not overlap inputs unless said otherwise.  A workspace belongs
+ * to one call at a time; nothing in it has to be kept or initialised.
+ * Errors: MALT_ERR_INVALID_ARG (null or inconsistent arguments, a workspace
+ * too small), MALT_ERR_UNSUPPORTED (types, sizes past the limits below),
+ * MALT_ERR_MISALIGNED, MALT_ERR_CUDA. */
+
+/* Embedding lookup with scaling, and the table's gradient.
+ *   forward:   rows[t] = scale * table[ids[t]]
+ *   backward:  table[v] = scale * sum over the t with ids[t] = v of rows[t]
+ * with table the vocab x dim matrix (backward: its gradient, every row
+ * written) and rows the tokens x dim one (backward: the gradient of the
+ * lookup's output).  With accumulate != 0 the backward call adds to what table
+ * holds (gradients of several micro-batches, or of a head tied to the table)
+ * and touches only the rows that occur.  A negative id is padding: its output
+ * row is zero and it adds nothing.  An id >= vocab is an error of the caller
+ * that costs no memory safety: its output row is NaN, and it adds nothing.
+ * Sums are fp32 in the order of the tokens, in windows of a length that
+ * depends on `tokens` only.  tokens, vocab, dim < 2^31 - 2^16. */
+typedef struct {
+    const void* ids;            /* tokens ids, MALT_I32 or MALT_I64          */
+    int32_t     ids_dtype;
+    int32_t     table_dtype;
+    int32_t     rows_dtype;
+    float       scale;
+    int64_t     tokens, vocab, dim;
+    void*       table;          /* forward: read; backward: written          */
+    int64_t     table_ld;       /* elements between two rows, >= dim         */
+    void*       rows;           /* forward: written; backward: read          */
+    int64_t     rows_ld;
+} malt_embed_t;
+int malt_embed_forward(const malt_embed_t* e, void* stream);
+size_t malt_embed_workspace_bytes(int64_t tokens, int64_t dim);
+int malt_embed_backward(const malt_embed_t* e, int32_t accumulate, void* workspace, size_t workspace_bytes,
+                        void* stream);
+
+/* RMS norms of queries and keys for each head, and the position rotation in
+ * the same pass.  Per head x (head_dim entries) of a token at position s:
+ *   n = x g / sqrt(mean(x^2) + eps),
+ *   y_a = n_a cos[s][i] - n_b sin[s][i],  y_b = n_b cos[s][i] + n_a sin[s][i]
+ * for the pairs (a, b) = (i, rot_dim/2 + i), or (2i, 2i+1) when interleaved,
+ * i < rot_dim/2; entries past rot_dim are n itself.  The gradient takes the
+ * same x and the gradients of y, and gives those of x and of the two gains
+ * (summed over batch, tokens and heads); nothing is kept between the calls.
+ * A position outside [0, table_rows) has no angle: the rotated entries of its
+ * rows, and what the gradient makes of them, are NaN.
+ * Each output may be its own input's buffer with the same strides (y = x;
+ * dx = dy or dx = x).  head_dim <= 1024, rot_dim even and <= head_dim,
+ * batch * seq < 2^31, heads < 2^20 (0 for none). */
+typedef struct {
+    int32_t      dtype;                  /* queries, keys, outputs and their gradients */
+    int32_t      gain_dtype;
+    int32_t      head_dim, rot_dim;
+    int32_t      interleaved;
+    float        eps;
+    int64_t      batch, seq;
+    const void*  positions;              /* [batch][seq], or NULL for 0 .. seq-1       */
+    int32_t      positions_dtype;        /* MALT_I32 or MALT_I64                       */
+    int32_t      pad_;
+    int64_t      positions_batch_stride; /* 0: the same positions for every sequence   */
+    const float* cosines;                /* [table_rows][rot_dim/2]                    */
+    const float* sines;
+    int64_t      table_rows;
+    const void*  q_gain;                 /* head_dim, or NULL for ones                 */
+    const void*  k_gain;
+} malt_qk_norm_t;
+/* [batch][seq][heads][head_dim] with these strides, entries of a head adjacent. */
+typedef struct {
+    void*   data;
+    int64_t heads, batch_stride, seq_stride, head_stride;
+} malt_heads_t;
+int malt_qk_norm_forward(const malt_qk_norm_t* p, const malt_heads_t* q, const malt_heads_t* k,
+                         const malt_heads_t* q_out, const malt_heads_t* k_out, void* stream);
+size_t malt_qk_norm_workspace_bytes(int32_t head_dim);
+/* dq_gain, dk_gain: head_dim floats each, or NULL where not wanted. */
+int malt_qk_norm_backward(const malt_qk_norm_t* p, const malt_heads_t* dq_out, const malt_heads_t* dk_out,
+                          const malt_heads_t* q, const malt_heads_t* k, const malt_heads_t* dq,
+                          const malt_heads_t* dk, float* dq_gain, float* dk_gain, void* workspace,
+                          size_t workspace_bytes, void* stream);
+
+/* Distillation from a teacher's top logits.  Per row, with the student's
+ * logits s over the vocabulary, the teacher's listed entries (id_j, t_j),
+ * temperature T and weight w:
+ *   p = softmax of t_j / T over the listed entries,  q = softmax(s / T),
+ *   loss = w T^2 sum_j p_j (log p_j - log q[id_j]),
+ *   dlogits_v = w T (q_v - sum over the j with id_j = v of p_j).
+ * Entries with an id outside [0, vocab) or a teacher logit of -inf are not
+ * listed (teachers that kept fewer); an id listed twice counts twice.  A row
+ * of weight 0 or with nothing listed has loss 0, statistics 0 and gradient 0
+ * whatever its logits hold; other rows propagate NaN and +inf.
+ * stats: 2 floats per row, the row's maximum m and sum_v exp((s_v - m) / T).
+ * malt_distill_forward writes the losses and (unless NULL) the statistics;
+ * malt_distill_backward takes the statistics and the gradient dloss of each
+ * row's loss (NULL: ones) and writes the gradient of the logits, in the
+ * logits' type; malt_distill_forward_backward does both at once for the sum of
+ * the losses (a mean is a weight of 1 / rows).  dlogits may be the logits'
+ * buffer with the same leading dimension.  top <= 1024, vocab < 2^31,
+ * rows < 2^27, T in [1e-15, 1e15]. */
+typedef struct {
+    const void*  logits;        /* rows x vocab                               */
+    int64_t      ld;            /* elements between two rows, >= vocab        */
+    int64_t      rows, vocab;
+    int32_t      dtype;         /* logits and their gradient                  */
+    int32_t      ids_dtype;     /* MALT_I32 or MALT_I64                       */
+    const void*  top_ids;       /* rows x top                                 */
+    int64_t      top_ids_ld;    /* elements between two rows, >= top          */
+    const void*  top_logits;    /* rows x top                                 */
+    int64_t      top_logits_ld;
+    int64_t      top;
+    const float* weight;        /* rows, or NULL for ones                     */
+    int32_t      top_dtype;     /* MALT_F32 or MALT_BF16                      */
+    float        temperature;
+} malt_distill_t;
+int malt_distill_forward(const malt_distill_t* d, float* loss, float* stats, void* stream);
+int malt_distill_backward(const malt_distill_t* d, const float* stats, const float* dloss, void* dlogits,
+                          int64_t dlogits_ld, void* stream);
+int malt_distill_forward_backward(const malt_distill_t* d, float* loss, float* stats, void* dlogits,
+                                  int64_t dlogits_ld, void* stream);
 
 /* Bytes of device workspace the state holds. */
 size_t malt_workspace_bytes(const malt_state_t* st);

@@ -1,0 +1,467 @@
+// embed.cu -- embedding lookup with scaling, and the table's gradient by sorted tokens.
+//
+// Forward:   out[t] = scale * table[ids[t]].
+// Backward:  dtable[v] (+)= scale * sum over the t with ids[t] = v of dout[t],
+// summed in fp32 in an order that the tokens alone fix: the tokens of a row in
+// their own order, long runs in windows of a fixed length.
+//
+// Both are bound by HBM.  The gradient is written once: rows that no token names
+// are zeroed by the sort launch, the others stored by the launch that sums them.
+#include <algorithm>
+
+#include <nvtx3/nvToolsExt.h>
+
+#include "model_ops.cuh"
+
+namespace malt {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kWarps = kThreads / 32;
+
+// ------------------------------------------------------------------- forward
+// One warp per token and slice of the row; every lane has up to kFwdLoads
+// vectors in flight.
+constexpr int kFwdLoads = 8;
+
+template <typename I>
+__device__ __forceinline__ int64_t load_id(const I* ids, int64_t t) {
+    return static_cast<int64_t>(ids[t]);
+}
+
+template <typename I, typename S, typename D, int VEC>
+__global__ void __launch_bounds__(kThreads)
+embed_forward_kernel(const I* ids, int64_t tokens, int64_t vocab, int64_t dim, const S* table, int64_t table_ld,
+                     D* out, int64_t out_ld, float scale, int steps, int slices) {
+    chain_wait();
+    const int lane = threadIdx.x & 31;
+    const int64_t item = static_cast<int64_t>(blockIdx.x) * kWarps + (threadIdx.x >> 5);
+    const int64_t t = item / slices;
+    if (t >= tokens) return;
+    const int64_t begin = (item - t * slices) * steps * (32 * VEC) + lane * VEC;
+    const int64_t id = load_id(ids, t);
+    D* const o = out + t * out_ld;
+    float x[kFwdLoads][VEC];
+    if (id >= 0 && id < vocab) {
+        const S* const row = table + id * table_ld;
+#pragma unroll
+        for (int j = 0; j < kFwdLoads; ++j) {
+            const int64_t e = begin + j * (32 * VEC);
+            if (j < steps && e < dim) load_vec<S, VEC>(row + e, x[j]);
+        }
+    } else {
+        // padding has no row; an id past the table has no value
+        const float v = id < 0 ? 0.f : __int_as_float(0x7fc00000);
+#pragma unroll
+        for (int j = 0; j < kFwdLoads; ++j)
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) x[j][i] = v;
+    }
+#pragma unroll
+    for (int j = 0; j < kFwdLoads; ++j) {
+        const int64_t e = begin + j * (32 * VEC);
+        if (j < steps && e < dim) {
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) x[j][i] *= scale;
+            store_vec<D, VEC>(o + e, x[j]);
+        }
+    }
+}
+
+// ------------------------------------------------------------ backward: sort
+// Block b owns the table rows [b R, (b + 1) R).  It reads every id, counts those
+// of its rows (per warp, each warp a contiguous run of tokens) and those below its
+// rows, and writes the records of its tokens to their place in the order (row,
+// token): no launch has to wait for another block's counts, and the order needs no
+// atomic that decides it.  Then it zeroes its rows that no token names.
+constexpr int kSortThreads = 1024;
+constexpr int kSortWarps = kSortThreads / 32;
+constexpr int kMaxOwned = kSortThreads;     // rows of a block: one thread scans each
+
+// A token in sorted order: its index, its row and the row's range of records.
+struct __align__(16) TokenRecord {
+    int32_t token, row, begin, end;
+};
+
+template <typename I, typename D, int VEC>
+__global__ void __launch_bounds__(kSortThreads)
+embed_sort_kernel(const I* ids, int32_t tokens, int32_t vocab, int32_t owned, TokenRecord* rec, int32_t* total,
+                  D* dtable, int64_t ld, int64_t dim, int fill) {
+    extern __shared__ uint32_t smem[];
+    uint32_t* const place = smem;                               // [kSortWarps][owned]
+    int32_t* const row_begin = reinterpret_cast<int32_t*>(smem + kSortWarps * owned);
+    int32_t* const row_end = row_begin + owned;
+    __shared__ int32_t warp_tmp[kSortWarps];
+    __shared__ int32_t s_base;
+
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int32_t v0 = static_cast<int32_t>(blockIdx.x) * owned;
+    const int32_t v1 = min(vocab, v0 + owned);
+    for (int i = threadIdx.x; i < kSortWarps * owned; i += kSortThreads) place[i] = 0;
+    __syncthreads();
+    chain_wait();
+
+    const int32_t per = (tokens / kSortWarps / 32 + 1) * 32;
+    const int32_t lo = static_cast<int32_t>(min(static_cast<int64_t>(warp) * per, static_cast<int64_t>(tokens)));
+    const int32_t hi = static_cast<int32_t>(min(static_cast<int64_t>(lo) + per, static_cast<int64_t>(tokens)));
+    uint32_t* const mine = place + warp * owned;
+    int32_t below = 0;
+#pragma unroll 4
+    for (int64_t i = lo + lane; i < hi; i += 32) {
+        const int64_t id = load_id(ids, i);
+        if (id >= 0 && id < v1) {
+            if (id < v0) ++below;
+            else atomicAdd(mine + (id - v0), 1u);
+        }
+    }
+    below = __reduce_add_sync(~0u, below);
+    if (lane == 0) warp_tmp[warp] = below;
+    __syncthreads();
+    if (warp == 0) {
+        const int32_t b = __reduce_add_sync(~0u, warp_tmp[lane]);
+        if (lane == 0) s_base = b;
+    }
+    __syncthreads();
+    // Exclusive sums: over the rows, and within a row over the warps.
+    int32_t count = 0;
+    if (threadIdx.x < owned)
+        for (int w = 0; w < kSortWarps; ++w) count += place[w * owned + threadIdx.x];
+    int32_t incl = count;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+        const int32_t up = __shfl_up_sync(~0u, incl, d);
+        if (lane >= d) incl += up;
+    }
+    if (lane == 31) warp_tmp[warp] = incl;
+    __syncthreads();
+    int32_t before = lane < warp ? warp_tmp[lane] : 0;
+    before = __reduce_add_sync(~0u, before);
+    if (threadIdx.x < owned) {
+        int32_t at = s_base + before + incl - count;
+        row_begin[threadIdx.x] = at;
+        row_end[threadIdx.x] = at + count;
+        for (int w = 0; w < kSortWarps; ++w) {
+            const int32_t n = place[w * owned + threadIdx.x];
+            place[w * owned + threadIdx.x] = at;
+            at += n;
+        }
+    }
+    if (blockIdx.x == gridDim.x - 1 && threadIdx.x == kSortThreads - 1) *total = s_base + before + incl;
+    __syncthreads();
+
+    for (int32_t i0 = lo; i0 < hi; i0 += 32) {
+        const int32_t i = i0 + lane;
+        const int64_t id = i < hi ? load_id(ids, i) : -1;
+        const bool in = id >= v0 && id < v1;
+        const unsigned m = __ballot_sync(~0u, in);
+        if (in) {
+            const int r = static_cast<int>(id - v0);
+            const unsigned peers = __match_any_sync(m, r);
+            const uint32_t first = mine[r];
+            __syncwarp(m);
+            if ((peers & ((1u << lane) - 1)) == 0) mine[r] = first + __popc(peers);
+            __syncwarp(m);
+            const uint32_t at = first + __popc(peers & ((1u << lane) - 1));
+            rec[at] = TokenRecord{i, static_cast<int32_t>(id), row_begin[r], row_end[r]};
+        }
+    }
+    if (!fill) return;
+    const float zero[VEC] = {};
+    for (int r = warp; r < v1 - v0; r += kSortWarps) {
+        if (row_begin[r] != row_end[r]) continue;
+        D* const row = dtable + static_cast<int64_t>(v0 + r) * ld;
+        for (int64_t e = lane * VEC; e < dim; e += 32 * VEC) store_vec<D, VEC>(row + e, zero);
+    }
+}
+
+// ------------------------------------------------------------- backward: sums
+// A warp takes a window of the sorted tokens and a slice of the row.  A row of at
+// most `window` tokens is summed by the window that it begins in, whole; a longer
+// one in parts, a part per window, which the join launch adds up.
+constexpr int kSumLoads = 8;        // tokens in flight
+
+template <typename D, int VEC, int SUB>
+__device__ __forceinline__ void store_row(D* row, int64_t base, int64_t dim, float (&acc)[SUB][VEC], float scale,
+                                          int accumulate) {
+#pragma unroll
+    for (int s = 0; s < SUB; ++s) {
+        const int64_t e = base + s * (32 * VEC);
+        if (e >= dim) continue;
+        float y[VEC];
+        if (accumulate) {
+            load_vec<D, VEC>(row + e, y);
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) y[i] = fmaf(scale, acc[s][i], y[i]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) y[i] = scale * acc[s][i];
+        }
+        store_vec<D, VEC>(row + e, y);
+    }
+}
+
+template <typename S, typename D, int VEC, int SUB>
+__global__ void __launch_bounds__(kThreads)
+embed_sum_kernel(const TokenRecord* rec, const int32_t* total, int32_t windows, int32_t window, int32_t slices,
+                 const S* dout, int64_t dout_ld, D* dtable, int64_t ld, int64_t dim, float scale, int accumulate,
+                 float* parts) {
+    chain_wait();
+    const int lane = threadIdx.x & 31;
+    const int64_t item = static_cast<int64_t>(blockIdx.x) * kWarps + (threadIdx.x >> 5);
+    const int32_t w = static_cast<int32_t>(item / slices);
+    if (w >= windows) return;
+    const int64_t base = (item - static_cast<int64_t>(w) * slices) * (32 * VEC * SUB) + lane * VEC;
+    const int32_t n = *after_wait(total);
+    const int32_t a = w * window, b = min(n, a + window);
+    if (a >= n) return;
+    rec = after_wait(rec);
+    int32_t i = a;
+    {
+        const TokenRecord first = rec[a];
+        if (first.begin < a && first.end - first.begin <= window) i = first.end;    // the window before has it
+    }
+    while (i < b) {
+        const TokenRecord head = rec[i];
+        const bool whole = head.end - head.begin <= window;
+        const int32_t end = whole ? head.end : min(head.end, b);
+        float acc[SUB][VEC] = {};
+        for (int32_t at = i; at < end; at += kSumLoads) {
+            float x[kSumLoads][SUB][VEC];
+#pragma unroll
+            for (int j = 0; j < kSumLoads; ++j) {
+                if (at + j < end) {
+                    const S* const row = dout + static_cast<int64_t>(rec[at + j].token) * dout_ld;
+#pragma unroll
+                    for (int s = 0; s < SUB; ++s) {
+                        const int64_t e = base + s * (32 * VEC);
+                        if (e < dim) load_vec<S, VEC>(row + e, x[j][s]);
+                    }
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < kSumLoads; ++j)
+                if (at + j < end)
+#pragma unroll
+                    for (int s = 0; s < SUB; ++s)
+#pragma unroll
+                        for (int k = 0; k < VEC; ++k) acc[s][k] += x[j][s][k];
+        }
+        if (whole) {
+            store_row<D, VEC, SUB>(dtable + static_cast<int64_t>(head.row) * ld, base, dim, acc, scale, accumulate);
+        } else {
+            // slot 0: the row began in an earlier window; slot 1: it begins in this one
+            float* const part = parts + (static_cast<int64_t>(w) * 2 + (head.begin >= a)) * dim;
+#pragma unroll
+            for (int s = 0; s < SUB; ++s)
+#pragma unroll
+                for (int k = 0; k < VEC; ++k) {
+                    const int64_t e = base + s * (32 * VEC) + k;
+                    if (e < dim) part[e] = acc[s][k];
+                }
+        }
+        i = end;
+    }
+}
+
+// The rows of more than `window` tokens: the parts of each added up by the block of
+// the window it begins in, a warp every kWarps-th part.
+template <typename D>
+__global__ void __launch_bounds__(kThreads)
+embed_join_kernel(const TokenRecord* rec, const int32_t* total, int32_t window, D* dtable, int64_t ld, int64_t dim,
+                  float scale, int accumulate, const float* parts) {
+    chain_wait();
+    const int32_t n = *after_wait(total);
+    const int32_t w = blockIdx.x;
+    const int32_t a = w * window, b = min(n, a + window);
+    if (a >= n) return;
+    const TokenRecord last = after_wait(rec)[b - 1];
+    if (last.end - last.begin <= window || last.begin < a) return;
+    parts = after_wait(parts);
+    const int32_t w_end = (last.end - 1) / window;
+    __shared__ float sums[kWarps][32];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    D* const row = dtable + static_cast<int64_t>(last.row) * ld;
+    for (int64_t e0 = 0; e0 < dim; e0 += 32) {
+        const int64_t e = e0 + lane;
+        float acc = 0.f;
+        if (e < dim) {
+            for (int32_t k = w + warp; k <= w_end; k += kWarps)
+                acc += parts[(static_cast<int64_t>(k) * 2 + (k == w)) * dim + e];
+        }
+        sums[warp][lane] = acc;
+        __syncthreads();
+        if (warp == 0 && e < dim) {
+            float y[1] = {0.f};
+#pragma unroll
+            for (int k = 0; k < kWarps; ++k) y[0] += sums[k][lane];
+            float old[1] = {0.f};
+            if (accumulate) load_vec<D, 1>(row + e, old);
+            y[0] = fmaf(scale, y[0], old[0]);
+            store_vec<D, 1>(row + e, y);
+        }
+        __syncthreads();
+    }
+}
+
+// ----------------------------------------------------------------------- host
+// Windows of the sorted tokens: 32 tokens, more where that would make over 1024
+// windows (a row's parts are then at most 1024).
+int32_t window_length(int64_t tokens) {
+    int64_t w = 32;
+    while (tokens > w * 1024) w *= 2;
+    return static_cast<int32_t>(w);
+}
+
+struct Workspace {
+    size_t rec, total, parts, bytes;
+};
+Workspace workspace_of(int64_t tokens, int64_t dim) {
+    const int64_t window = window_length(tokens), windows = (tokens + window - 1) / window;
+    Workspace w;
+    w.rec = 0;
+    w.total = static_cast<size_t>(tokens) * sizeof(TokenRecord);
+    w.parts = w.total + 256;
+    w.bytes = w.parts + (tokens > window ? static_cast<size_t>(windows) * 2 * dim * sizeof(float) : 0);
+    return w;
+}
+
+int check(const malt_embed_t* e) {
+    if (e == nullptr || e->tokens < 0 || e->vocab < 0 || e->dim < 0 || !(e->scale == e->scale))
+        return MALT_ERR_INVALID_ARG;
+    if (!index_type(e->ids_dtype) || !float_type(e->table_dtype) || !float_type(e->rows_dtype))
+        return MALT_ERR_UNSUPPORTED;
+    constexpr int64_t kMax = (int64_t{1} << 31) - 1 - (1 << 16);
+    if (e->tokens > kMax || e->vocab > kMax || e->dim > kMax) return MALT_ERR_UNSUPPORTED;
+    if (e->table_ld < e->dim || e->rows_ld < e->dim) return MALT_ERR_INVALID_ARG;
+    if ((e->tokens > 0 && (e->ids == nullptr || (e->dim > 0 && e->rows == nullptr))) ||
+        (e->vocab > 0 && e->dim > 0 && e->table == nullptr))
+        return MALT_ERR_INVALID_ARG;
+    if (!aligned_to(e->ids, type_bytes(e->ids_dtype)) || !aligned_to(e->table, type_bytes(e->table_dtype)) ||
+        !aligned_to(e->rows, type_bytes(e->rows_dtype)))
+        return MALT_ERR_MISALIGNED;
+    return MALT_OK;
+}
+
+// Whether both matrices can be read and written in vectors of vec elements.
+bool vectors(const malt_embed_t* e, int vec) {
+    const int tb = type_bytes(e->table_dtype) * vec, rb = type_bytes(e->rows_dtype) * vec;
+    return e->dim % vec == 0 && e->table_ld % vec == 0 && e->rows_ld % vec == 0 &&
+           aligned_to(e->table, std::min(tb, 16)) && aligned_to(e->rows, std::min(rb, 16));
+}
+
+template <typename I, typename S, typename D, int VEC>
+cudaError_t forward(const malt_embed_t* e, cudaStream_t s) {
+    const int64_t all = (e->dim + 32 * VEC - 1) / (32 * VEC);
+    const int64_t slices = (all + kFwdLoads - 1) / kFwdLoads;
+    const int64_t steps = (all + slices - 1) / slices;
+    const int64_t blocks = (e->tokens * slices + kWarps - 1) / kWarps;
+    if (blocks >= (int64_t{1} << 31)) return cudaErrorInvalidValue;
+    return launch_chained(embed_forward_kernel<I, S, D, VEC>, static_cast<unsigned>(blocks), kThreads, 0, s,
+                          static_cast<const I*>(e->ids), e->tokens, e->vocab, e->dim,
+                          static_cast<const S*>(e->table), e->table_ld, static_cast<D*>(e->rows), e->rows_ld,
+                          e->scale, static_cast<int>(steps), static_cast<int>(slices));
+}
+
+template <typename I, typename D, int VEC>
+cudaError_t sort(const malt_embed_t* e, const Workspace& w, uint8_t* ws, int fill, cudaStream_t s) {
+    const int64_t blocks0 = std::max<int64_t>(sm_count(), (e->vocab + kMaxOwned - 1) / kMaxOwned);
+    const int32_t owned = static_cast<int32_t>((e->vocab + blocks0 - 1) / blocks0);
+    const unsigned blocks = static_cast<unsigned>((e->vocab + owned - 1) / owned);
+    const size_t smem = (kSortWarps + 2) * sizeof(uint32_t) * static_cast<size_t>(owned);
+    auto* const kernel = embed_sort_kernel<I, D, VEC>;
+    if (smem > 48 * 1024) {
+        const cudaError_t rc = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                                    static_cast<int>(smem));
+        if (rc != cudaSuccess) { cudaGetLastError(); return rc; }
+    }
+    return launch_chained(kernel, blocks, kSortThreads, smem, s, static_cast<const I*>(e->ids),
+                          static_cast<int32_t>(e->tokens), static_cast<int32_t>(e->vocab), owned,
+                          reinterpret_cast<TokenRecord*>(ws + w.rec), reinterpret_cast<int32_t*>(ws + w.total),
+                          static_cast<D*>(e->table), e->table_ld, e->dim, fill);
+}
+
+template <typename S, typename D, int VEC, int SUB>
+cudaError_t sums(const malt_embed_t* e, const Workspace& w, uint8_t* ws, int accumulate, cudaStream_t s) {
+    const int32_t window = window_length(e->tokens);
+    const int32_t windows = static_cast<int32_t>((e->tokens + window - 1) / window);
+    const int64_t slices = (e->dim + 32 * VEC * SUB - 1) / (32 * VEC * SUB);
+    const int64_t blocks = (windows * slices + kWarps - 1) / kWarps;
+    if (blocks >= (int64_t{1} << 31)) return cudaErrorInvalidValue;
+    const TokenRecord* const rec = reinterpret_cast<TokenRecord*>(ws + w.rec);
+    const int32_t* const total = reinterpret_cast<int32_t*>(ws + w.total);
+    float* const parts = reinterpret_cast<float*>(ws + w.parts);
+    D* const dtable = static_cast<D*>(e->table);
+    cudaError_t rc = launch_chained(embed_sum_kernel<S, D, VEC, SUB>, static_cast<unsigned>(blocks), kThreads, 0, s,
+                                    rec, total, windows, window, static_cast<int32_t>(slices),
+                                    static_cast<const S*>(e->rows), e->rows_ld, dtable, e->table_ld, e->dim,
+                                    e->scale, accumulate, parts);
+    if (rc != cudaSuccess || e->tokens <= window) return rc;
+    return launch_chained(embed_join_kernel<D>, static_cast<unsigned>(windows), kThreads, 0, s, rec, total, window,
+                          dtable, e->table_ld, e->dim, e->scale, accumulate, static_cast<const float*>(parts));
+}
+
+template <typename I>
+cudaError_t forward_types(const malt_embed_t* e, cudaStream_t s) {
+    const bool tb = e->table_dtype == MALT_BF16, rb = e->rows_dtype == MALT_BF16;
+    if (tb && rb) return vectors(e, 8) ? forward<I, bf16, bf16, 8>(e, s) : forward<I, bf16, bf16, 1>(e, s);
+    if (tb) return vectors(e, 4) ? forward<I, bf16, float, 4>(e, s) : forward<I, bf16, float, 1>(e, s);
+    if (rb) return vectors(e, 4) ? forward<I, float, bf16, 4>(e, s) : forward<I, float, bf16, 1>(e, s);
+    return vectors(e, 4) ? forward<I, float, float, 4>(e, s) : forward<I, float, float, 1>(e, s);
+}
+
+template <typename I, typename D>
+cudaError_t sort_types(const malt_embed_t* e, const Workspace& w, uint8_t* ws, int fill, cudaStream_t s) {
+    constexpr int V = 16 / sizeof(D);
+    return e->table_ld % V == 0 && e->dim % V == 0 && aligned_to(e->table, 16) ? sort<I, D, V>(e, w, ws, fill, s)
+                                                                                : sort<I, D, 1>(e, w, ws, fill, s);
+}
+
+template <typename S, typename D>
+cudaError_t sums_types(const malt_embed_t* e, const Workspace& w, uint8_t* ws, int accumulate, cudaStream_t s) {
+    return vectors(e, 4) ? sums<S, D, 4, 2>(e, w, ws, accumulate, s) : sums<S, D, 1, 4>(e, w, ws, accumulate, s);
+}
+
+}  // namespace
+}  // namespace malt
+
+extern "C" {
+
+int malt_embed_forward(const malt_embed_t* e, void* stream) {
+    using namespace malt;
+    const int rc = check(e);
+    if (rc != MALT_OK || e->tokens == 0 || e->dim == 0) return rc;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    nvtxRangePushA("malt_embed_forward");
+    const cudaError_t c = e->ids_dtype == MALT_I32 ? forward_types<int32_t>(e, s) : forward_types<int64_t>(e, s);
+    nvtxRangePop();
+    return cuda_status(c, "malt_embed_forward");
+}
+
+size_t malt_embed_workspace_bytes(int64_t tokens, int64_t dim) {
+    if (tokens < 0 || dim < 0) return 0;
+    return malt::workspace_of(tokens, dim).bytes;
+}
+
+int malt_embed_backward(const malt_embed_t* e, int32_t accumulate, void* workspace, size_t workspace_bytes,
+                        void* stream) {
+    using namespace malt;
+    const int rc = check(e);
+    if (rc != MALT_OK || e->vocab == 0 || e->dim == 0 || (accumulate && e->tokens == 0)) return rc;
+    const Workspace w = workspace_of(e->tokens, e->dim);
+    if (workspace == nullptr || workspace_bytes < w.bytes) return MALT_ERR_INVALID_ARG;
+    if (!aligned_to(workspace, 16)) return MALT_ERR_MISALIGNED;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    uint8_t* const ws = static_cast<uint8_t*>(workspace);
+    nvtxRangePushA("malt_embed_backward");
+    const int fill = accumulate ? 0 : 1;
+    const bool i32 = e->ids_dtype == MALT_I32, tb = e->table_dtype == MALT_BF16, rb = e->rows_dtype == MALT_BF16;
+    cudaError_t c = i32 ? (tb ? sort_types<int32_t, bf16>(e, w, ws, fill, s) : sort_types<int32_t, float>(e, w, ws, fill, s))
+                        : (tb ? sort_types<int64_t, bf16>(e, w, ws, fill, s) : sort_types<int64_t, float>(e, w, ws, fill, s));
+    if (c == cudaSuccess && e->tokens > 0)
+        c = rb ? (tb ? sums_types<bf16, bf16>(e, w, ws, accumulate != 0, s) : sums_types<bf16, float>(e, w, ws, accumulate != 0, s))
+               : (tb ? sums_types<float, bf16>(e, w, ws, accumulate != 0, s) : sums_types<float, float>(e, w, ws, accumulate != 0, s));
+    nvtxRangePop();
+    return cuda_status(c, "malt_embed_backward");
+}
+
+}  // extern "C"

@@ -28,6 +28,8 @@ MALT_ERR_TIMEOUT = -6
 MALT_ERR_OUT_OF_MEMORY = -7
 MALT_F32 = 0
 MALT_BF16 = 1
+MALT_I32 = 2
+MALT_I64 = 3
 SCALARS_PER_MAT = 8
 
 # Exported entry points declared in include/malt.h.
@@ -40,7 +42,9 @@ EXPORTS = ("malt_init_state", "malt_step", "malter_step", "malt_get_scalars",
            "malt_set_weight_copies", "malt_adamw_init_state", "malt_adamw_step",
            "malt_adamw_get_step", "malt_adamw_set_step", "malt_adamw_destroy_state",
            "malt_debug_check_guards", "malt_ns_plan", "malt_muon_ns_plan",
-           "malt_ns_tables")
+           "malt_ns_tables", "malt_embed_forward", "malt_embed_workspace_bytes", "malt_embed_backward",
+           "malt_qk_norm_forward", "malt_qk_norm_workspace_bytes", "malt_qk_norm_backward",
+           "malt_distill_forward", "malt_distill_backward", "malt_distill_forward_backward")
 NOALLOC_SCRATCH_FLOATS = 1048576
 KIND_NAMES = ("bind", "stats", "finalize", "prescale", "norms", "ns_gram", "ns_poly", "ns_bx",
               "scalars", "apply", "ns_persistent", "pad")
@@ -160,6 +164,22 @@ def load(build_if_missing: bool = False) -> ctypes.CDLL:
     lib.malt_ns_tables.restype = ctypes.c_int
     for name in ("malt_ns_plan", "malt_muon_ns_plan"):
         getattr(lib, name).argtypes = [i64, i64, i32, P(malt_hparams_t), P(malt_ns_op_t), i32, P(i32)]
+        getattr(lib, name).restype = ctypes.c_int
+    # model operators: their structs are packed by model_ops.py
+    sz = ctypes.c_size_t
+    lib.malt_embed_forward.argtypes = [vp, vp]
+    lib.malt_embed_workspace_bytes.argtypes = [i64, i64]
+    lib.malt_embed_workspace_bytes.restype = sz
+    lib.malt_embed_backward.argtypes = [vp, i32, vp, sz, vp]
+    lib.malt_qk_norm_forward.argtypes = [vp] * 6
+    lib.malt_qk_norm_workspace_bytes.argtypes = [i32]
+    lib.malt_qk_norm_workspace_bytes.restype = sz
+    lib.malt_qk_norm_backward.argtypes = [vp] * 10 + [sz, vp]
+    lib.malt_distill_forward.argtypes = [vp] * 4
+    lib.malt_distill_backward.argtypes = [vp] * 4 + [i64, vp]
+    lib.malt_distill_forward_backward.argtypes = [vp] * 4 + [i64, vp]
+    for name in ("malt_embed_forward", "malt_embed_backward", "malt_qk_norm_forward", "malt_qk_norm_backward",
+                 "malt_distill_forward", "malt_distill_backward", "malt_distill_forward_backward"):
         getattr(lib, name).restype = ctypes.c_int
     for name in ("malt_init_state", "malt_step", "malter_step", "malt_get_scalars",
                  "malt_set_scalars", "malt_check", "malt_debug_direction",
