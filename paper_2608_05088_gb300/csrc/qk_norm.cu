@@ -40,6 +40,9 @@ struct Kind {           // queries or keys
     float* parts;       // [blocks][dim] partial gain gradients
     int32_t heads;
     int32_t blocks;
+    uint32_t split;     // slots of a token: slot j takes heads j, j + split, ...
+    uint32_t slots;     // of all tokens
+    int32_t gain_vectors;   // the gains are fp32 and aligned to 16 bytes
 };
 
 struct Params {
@@ -77,6 +80,238 @@ __device__ __forceinline__ float2 angle(const Params& P, int64_t pos, int p) {
     if (pos < 0 || pos >= P.table_rows) return make_float2(__int_as_float(0x7fc00000), __int_as_float(0x7fc00000));
     const int64_t i = pos * (P.rot / 2) + p;
     return make_float2(P.cosines[i], P.sines[i]);
+}
+
+// --------------------------------------------------------------- aligned rows
+// A row is held by LPR neighbouring lanes, 2 V entries each (V: 16 bytes of them):
+// the V pairs that the lane turns, partners in the lane, so that one lane needs V
+// cosines and V sines.  These lanes are a slot, which keeps its token's angles and
+// the gains in registers and walks over heads; neighbouring slots take neighbouring
+// heads of a token, so that a warp's loads are contiguous.
+template <typename T, bool INTER>
+struct Chunk {
+    static constexpr int V = 16 / sizeof(T);
+    int a, b;           // first entries of the lane's two vectors
+    bool turned;
+    __device__ __forceinline__ Chunk(int c, int rot) {
+        turned = c * 2 * V < rot;
+        if (INTER || !turned) {
+            a = c * 2 * V;
+            b = a + V;
+        } else {
+            a = c * V;
+            b = rot / 2 + c * V;
+        }
+    }
+    // entry of the lane's value i of 2 V, and the two values of its pair p
+    __device__ __forceinline__ int entry(int i) const { return i < V ? a + i : b + i - V; }
+    static __device__ __forceinline__ constexpr int first(int p) { return INTER ? 2 * p : p; }
+    static __device__ __forceinline__ constexpr int second(int p) { return INTER ? 2 * p + 1 : V + p; }
+};
+
+template <int V>
+struct Angles {
+    float c[V], s[V];
+    __device__ __forceinline__ void load(const Params& P, int64_t pos, int chunk, bool turned) {
+        const bool in = pos >= 0 && pos < P.table_rows;
+        if (turned && in) {
+            const int64_t at = pos * (P.rot / 2) + chunk * V;
+            load_vec<float, V>(P.cosines + at, c);
+            load_vec<float, V>(P.sines + at, s);
+        } else {
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                c[i] = turned ? __int_as_float(0x7fc00000) : 1.f;
+                s[i] = turned ? __int_as_float(0x7fc00000) : 0.f;
+            }
+        }
+    }
+};
+
+template <int LPR>
+__device__ __forceinline__ float row_sum(float v) {
+#pragma unroll
+    for (int d = LPR / 2; d > 0; d >>= 1) v += __shfl_xor_sync(~0u, v, d);
+    return v;
+}
+
+template <typename T>
+__device__ __forceinline__ uint4 load16(const T* p) { return *reinterpret_cast<const uint4*>(p); }
+
+// Gains of the lane's entries.
+template <typename C, int N>
+__device__ __forceinline__ void load_gains(const Params& P, const Kind& K, const C& chunk, float (&g)[N]) {
+    constexpr int V = N / 2;
+    if (K.gain_vectors) {
+        float lo[V], hi[V];
+        load_vec<float, V>(static_cast<const float*>(K.gain) + chunk.a, lo);
+        load_vec<float, V>(static_cast<const float*>(K.gain) + chunk.b, hi);
+#pragma unroll
+        for (int i = 0; i < V; ++i) g[i] = lo[i], g[V + i] = hi[i];
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) g[i] = gain_at(P, K, chunk.entry(i));
+    }
+}
+
+constexpr int kFwdHeads = 4;        // rows of a slot in flight
+constexpr int kBwdHeads = 2;
+
+template <typename T, bool INTER, int LPR>
+__global__ void __launch_bounds__(kThreads)
+qk_forward_kernel(const __grid_constant__ Params P) {
+    using C = Chunk<T, INTER>;
+    constexpr int V = C::V, N = 2 * V, U = kFwdHeads;
+    const bool keys = blockIdx.x >= P.kind[0].blocks;
+    const Kind& K = P.kind[keys];
+    const uint32_t block = blockIdx.x - (keys ? P.kind[0].blocks : 0);
+    const int lane = threadIdx.x & 31, sub = lane % LPR;
+    const uint32_t slot = (block * kWarps + (threadIdx.x >> 5)) * (32 / LPR) + lane / LPR;
+    const bool live = slot < K.slots && sub * N < P.dim;
+    const uint32_t token = slot / K.split, j = slot - token * K.split;
+    const int64_t b = token / static_cast<uint32_t>(P.seq), s = token - b * P.seq;
+    const C chunk(sub, P.rot);
+    const T* const x = static_cast<const T*>(K.x.data) + K.x.at(b, s, 0);
+    T* const y = static_cast<T*>(K.y.data) + K.y.at(b, s, 0);
+    float g[N];
+    Angles<V> t;
+    chain_wait();
+    for (int h0 = 0; h0 < K.heads; h0 += U * K.split) {
+        uint4 raw[U][2];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int h = h0 + u * K.split + j;
+            raw[u][0] = raw[u][1] = make_uint4(0, 0, 0, 0);
+            if (live && h < K.heads) {
+                raw[u][0] = load16(x + h * K.x.head_stride + chunk.a);
+                raw[u][1] = load16(x + h * K.x.head_stride + chunk.b);
+            }
+        }
+        if (h0 == 0 && live) {
+            t.load(P, position_of(P, b, s), sub, chunk.turned);
+            load_gains(P, K, chunk, g);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int h = h0 + u * K.split + j;
+            float v[N];
+            unpack<T>(raw[u][0], v);
+            unpack<T>(raw[u][1], v + V);
+            float ss = 0.f;
+#pragma unroll
+            for (int i = 0; i < N; ++i) ss = fmaf(v[i], v[i], ss);
+            const float r = rsqrtf(row_sum<LPR>(ss) / static_cast<float>(P.dim) + P.eps);
+            if (!live || h >= K.heads) continue;
+#pragma unroll
+            for (int i = 0; i < N; ++i) v[i] *= r * g[i];
+            float o[2][V];
+#pragma unroll
+            for (int p = 0; p < V; ++p) {
+                const int ia = C::first(p), ib = C::second(p);
+                o[ia / V][ia % V] = v[ia] * t.c[p] - v[ib] * t.s[p];
+                o[ib / V][ib % V] = v[ib] * t.c[p] + v[ia] * t.s[p];
+            }
+            store_vec<T, V>(y + h * K.y.head_stride + chunk.a, o[0]);
+            store_vec<T, V>(y + h * K.y.head_stride + chunk.b, o[1]);
+        }
+    }
+}
+
+// The blocks stay and walk over the slots, with the gain gradient of their lanes'
+// entries in registers; each leaves its sum for the join launch.
+template <typename T, bool INTER, int LPR>
+__global__ void __launch_bounds__(kThreads, 2)
+qk_backward_kernel(const __grid_constant__ Params P) {
+    using C = Chunk<T, INTER>;
+    constexpr int V = C::V, N = 2 * V, U = kBwdHeads, kSlots = 32 / LPR;
+    extern __shared__ float sums[];         // [kWarps][dim]
+    const bool keys = blockIdx.x >= P.kind[0].blocks;
+    const Kind& K = P.kind[keys];
+    const uint32_t block = blockIdx.x - (keys ? P.kind[0].blocks : 0);
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, sub = lane % LPR;
+    const bool mine = sub * N < P.dim;
+    const C chunk(sub, P.rot);
+    float g[N], acc[N] = {};
+    Angles<V> t;
+    chain_wait();
+    if (mine) load_gains(P, K, chunk, g);
+    const float n = static_cast<float>(P.dim);
+    for (uint64_t first = (static_cast<uint64_t>(block) * kWarps + warp) * kSlots; first < K.slots;
+         first += static_cast<uint64_t>(K.blocks) * kWarps * kSlots) {
+        const uint64_t slot = first + lane / LPR;
+        const bool live = slot < K.slots && mine;
+        const uint32_t token = static_cast<uint32_t>(slot) / K.split, j = static_cast<uint32_t>(slot) - token * K.split;
+        const int64_t b = token / static_cast<uint32_t>(P.seq), s = token - b * P.seq;
+        const T* const x = static_cast<const T*>(K.x.data) + K.x.at(b, s, 0);
+        const T* const dy = static_cast<const T*>(K.dy.data) + K.dy.at(b, s, 0);
+        T* const dx = static_cast<T*>(K.dx.data) + K.dx.at(b, s, 0);
+        for (int h0 = 0; h0 < K.heads; h0 += U * K.split) {
+            uint4 rx[U][2], ry[U][2];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int h = h0 + u * K.split + j;
+                rx[u][0] = rx[u][1] = ry[u][0] = ry[u][1] = make_uint4(0, 0, 0, 0);
+                if (live && h < K.heads) {
+                    rx[u][0] = load16(x + h * K.x.head_stride + chunk.a);
+                    rx[u][1] = load16(x + h * K.x.head_stride + chunk.b);
+                    ry[u][0] = load16(dy + h * K.dy.head_stride + chunk.a);
+                    ry[u][1] = load16(dy + h * K.dy.head_stride + chunk.b);
+                }
+            }
+            if (h0 == 0 && live) t.load(P, position_of(P, b, s), sub, chunk.turned);
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int h = h0 + u * K.split + j;
+                const bool here = live && h < K.heads;
+                float v[N], d[N];
+                unpack<T>(rx[u][0], v);
+                unpack<T>(rx[u][1], v + V);
+                unpack<T>(ry[u][0], d);
+                unpack<T>(ry[u][1], d + V);
+                float ss = 0.f, ux = 0.f;
+                if (here) {
+#pragma unroll
+                    for (int p = 0; p < V; ++p) {       // rotated back
+                        const int ia = C::first(p), ib = C::second(p);
+                        const float da = d[ia] * t.c[p] + d[ib] * t.s[p], db = d[ib] * t.c[p] - d[ia] * t.s[p];
+                        d[ia] = da;
+                        d[ib] = db;
+                    }
+#pragma unroll
+                    for (int i = 0; i < N; ++i) {
+                        ss = fmaf(v[i], v[i], ss);
+                        ux = fmaf(d[i] * g[i], v[i], ux);
+                    }
+                }
+                const float r = rsqrtf(row_sum<LPR>(ss) / n + P.eps);
+                const float c = r * r * (row_sum<LPR>(ux) / n);
+                if (!here) continue;
+                float o[2][V];
+#pragma unroll
+                for (int i = 0; i < N; ++i) {
+                    acc[i] = fmaf(d[i], v[i] * r, acc[i]);
+                    o[i / V][i % V] = r * (d[i] * g[i] - v[i] * c);
+                }
+                store_vec<T, V>(dx + h * K.dx.head_stride + chunk.a, o[0]);
+                store_vec<T, V>(dx + h * K.dx.head_stride + chunk.b, o[1]);
+            }
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+        for (int d = LPR; d < 32; d <<= 1) acc[i] += __shfl_xor_sync(~0u, acc[i], d);
+    if (lane < LPR && mine) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) sums[warp * P.dim + chunk.entry(i)] = acc[i];
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < P.dim; i += kThreads) {
+        float t = 0.f;
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) t += sums[w * P.dim + i];
+        K.parts[block * static_cast<int64_t>(P.dim) + i] = t;
+    }
 }
 
 // ------------------------------------------------------- any size and alignment
@@ -278,8 +513,84 @@ Params params_of(const malt_qk_norm_t* p) {
 int32_t backward_blocks() { return sm_count() * 6; }
 int32_t backward_parts() { return backward_blocks() + 2; }
 
+// Whether the rows of a view can be read in 16-byte vectors.
+template <typename T>
+bool vectors(const Params& P, const Rows& r) {
+    constexpr int64_t V = 16 / sizeof(T);
+    return aligned_to(r.data, 16) && (P.batch == 1 || r.batch_stride % V == 0) &&
+           (P.seq == 1 || r.seq_stride % V == 0) && r.head_stride % V == 0;
+}
+
+// Lanes of a row in the aligned kernels, 0 where they do not apply.
+template <typename T>
+int lanes_of(const Params& P, bool backward) {
+    constexpr int N = 32 / sizeof(T);
+    if (P.dim % N != 0 || P.rot % N != 0 || P.dim / N > 32) return 0;
+    if (!aligned_to(P.cosines, 16) || !aligned_to(P.sines, 16)) return 0;
+    for (const Kind& K : P.kind) {
+        if (K.heads == 0) continue;
+        if (!vectors<T>(P, K.x)) return 0;
+        if (backward ? !vectors<T>(P, K.dy) || !vectors<T>(P, K.dx) : !vectors<T>(P, K.y)) return 0;
+    }
+    int lanes = 2;
+    while (lanes * N < P.dim) lanes *= 2;
+    return lanes;
+}
+
+// Slots of a token for each kind: a few batches of heads a slot, which spreads the
+// angles' cost, but enough slots to fill the GPU.
+void split_heads(Params& P, int lanes, int batch) {
+    const int64_t tokens = P.batch * P.seq;
+    const int64_t wanted = sm_count() * 64ll * (32 / lanes);
+    for (Kind& K : P.kind) {
+        K.gain_vectors = K.gain != nullptr && !P.gain_bf16 && aligned_to(K.gain, 16);
+        int64_t rounds = 2, split;
+        do {
+            split = std::max<int64_t>(1, (K.heads + batch * rounds - 1) / (batch * rounds));
+        } while (--rounds > 0 && tokens * split < wanted);
+        if (tokens * K.heads < wanted) split = std::max(K.heads, 1);
+        if (tokens * split >= (int64_t{1} << 31)) split = 1;
+        K.split = static_cast<uint32_t>(split);
+        K.slots = K.heads == 0 ? 0 : static_cast<uint32_t>(tokens * split);
+    }
+}
+
+template <typename T, bool INTER, int LPR>
+cudaError_t forward_rows(Params& P, cudaStream_t s) {
+    constexpr int64_t kSlots = kWarps * (32 / LPR);
+    for (Kind& K : P.kind) K.blocks = static_cast<int32_t>((K.slots + kSlots - 1) / kSlots);
+    return launch_chained(qk_forward_kernel<T, INTER, LPR>, P.kind[0].blocks + P.kind[1].blocks, kThreads, 0, s, P);
+}
+
+template <typename T, bool INTER, int LPR>
+cudaError_t backward_rows(Params& P, cudaStream_t s) {
+    constexpr int64_t kSlots = kWarps * (32 / LPR);
+    const int64_t heads = P.kind[0].heads + P.kind[1].heads;
+    for (Kind& K : P.kind) {
+        const int64_t share = K.heads > 0 ? std::max<int64_t>(1, static_cast<int64_t>(sm_count()) * 2 * K.heads / heads) : 0;
+        K.blocks = static_cast<int32_t>(std::min<int64_t>((K.slots + kSlots - 1) / kSlots, share));
+    }
+    P.kind[1].parts = P.kind[0].parts + static_cast<int64_t>(P.kind[0].blocks) * P.dim;
+    return launch_chained(qk_backward_kernel<T, INTER, LPR>, P.kind[0].blocks + P.kind[1].blocks, kThreads,
+                          kWarps * P.dim * sizeof(float), s, P);
+}
+
+template <typename T, bool INTER>
+cudaError_t rows_kernel(Params& P, int lanes, bool backward, cudaStream_t s) {
+    split_heads(P, lanes, backward ? kBwdHeads : kFwdHeads);
+    switch (lanes) {
+        case 2: return backward ? backward_rows<T, INTER, 2>(P, s) : forward_rows<T, INTER, 2>(P, s);
+        case 4: return backward ? backward_rows<T, INTER, 4>(P, s) : forward_rows<T, INTER, 4>(P, s);
+        case 8: return backward ? backward_rows<T, INTER, 8>(P, s) : forward_rows<T, INTER, 8>(P, s);
+        case 16: return backward ? backward_rows<T, INTER, 16>(P, s) : forward_rows<T, INTER, 16>(P, s);
+        default: return backward ? backward_rows<T, INTER, 32>(P, s) : forward_rows<T, INTER, 32>(P, s);
+    }
+}
+
 template <typename T>
 cudaError_t forward(Params& P, bool inter, cudaStream_t s) {
+    if (const int lanes = lanes_of<T>(P, false))
+        return inter ? rows_kernel<T, true>(P, lanes, false, s) : rows_kernel<T, false>(P, lanes, false, s);
     for (Kind& K : P.kind) {
         const int64_t blocks = (P.batch * P.seq * K.heads + kWarps - 1) / kWarps;
         if (blocks >= (int64_t{1} << 30)) return cudaErrorInvalidValue;
@@ -291,6 +602,8 @@ cudaError_t forward(Params& P, bool inter, cudaStream_t s) {
 
 template <typename T>
 cudaError_t backward(Params& P, bool inter, cudaStream_t s) {
+    if (const int lanes = lanes_of<T>(P, true))
+        return inter ? rows_kernel<T, true>(P, lanes, true, s) : rows_kernel<T, false>(P, lanes, true, s);
     const int64_t heads = P.kind[0].heads + P.kind[1].heads;
     for (Kind& K : P.kind) {
         const int64_t blocks = (P.batch * P.seq * K.heads + kWarps - 1) / kWarps;
