@@ -10,11 +10,15 @@
 // whatever its logits hold.
 //
 // A thread block takes a row, or a cluster of blocks where there are few rows.  One
-// sweep finds the row's maximum m and sum of 2^((s - m) log2(e) / tau), each thread
-// with a running maximum over batches of vectors; the second writes the gradient and
-// finds the row in L2.  Bound by HBM: the logits once, their gradient once.
-// Differences are taken before the product with log2(e) / tau, so that a row of the
-// type's lowest values is a uniform one and not an overflow.
+// sweep finds the row's maximum m and sum of 2^((s - m) c), c = log2(e) / tau, each
+// thread with a running maximum over batches of vectors; the second writes the
+// gradient and finds the row in L2.  One warp more takes the teacher's entries
+// meanwhile.  Bound by HBM: the logits once, their gradient once.
+//
+// An exponent s c - m c is one fused multiply-add of the rounded product m c, whose
+// rounding is the same for every entry and is taken out of the sum again at its end.
+// Where that product leaves fp32's range (a row of the type's lowest values is a
+// uniform one) the difference is taken first.
 #include <algorithm>
 #include <cooperative_groups.h>
 
@@ -25,9 +29,8 @@
 namespace malt {
 namespace {
 
-constexpr int kThreads = 512;
-constexpr int kWarps = kThreads / 32;
 constexpr int kMaxTop = 1024;
+constexpr int kWide = 512, kNarrow = 128;      // threads that sweep a row
 constexpr int kBatch = 4;           // vectors of a thread in flight
 constexpr int kMaxCluster = 8;
 constexpr float kLog2e = 1.4426950408889634f;
@@ -61,29 +64,92 @@ __device__ __forceinline__ MaxSum merge(MaxSum a, MaxSum b, float c) {
     return MaxSum{m, a.s * rescale(a.m, m, c) + b.s * rescale(b.m, m, c)};
 }
 
-__device__ __forceinline__ float block_sum(float v, float* tmp) {
-    v = warp_sum(v);
-    __syncthreads();
-    if ((threadIdx.x & 31) == 0) tmp[threadIdx.x >> 5] = v;
-    __syncthreads();
-    return warp_sum((threadIdx.x & 31) < kWarps ? tmp[threadIdx.x & 31] : 0.f);
+// One vector of logits (16 bytes) as pairs of fp32, and its largest entry.
+template <typename T>
+__device__ __forceinline__ f32x2 pair_of(const uint4& u, int i) {
+    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+    if constexpr (sizeof(T) == 4) return pack2(__uint_as_float(w[2 * i]), __uint_as_float(w[2 * i + 1]));
+    else return pack2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u));
 }
-__device__ __forceinline__ float block_max(float v, float* tmp) {
-    v = warp_max(v);
-    __syncthreads();
-    if ((threadIdx.x & 31) == 0) tmp[threadIdx.x >> 5] = v;
-    __syncthreads();
-    return warp_max((threadIdx.x & 31) < kWarps ? tmp[threadIdx.x & 31] : -INFINITY);
+template <typename T, int N>
+__device__ __forceinline__ float largest(const uint4 (&u)[N]) {
+    if constexpr (sizeof(T) == 4) {
+        float m = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            m = fmaxf(m, fmaxf(fmaxf(__uint_as_float(u[i].x), __uint_as_float(u[i].y)),
+                               fmaxf(__uint_as_float(u[i].z), __uint_as_float(u[i].w))));
+        return m;
+    } else {
+        auto h = [](uint32_t w) { return *reinterpret_cast<const __nv_bfloat162*>(&w); };
+        __nv_bfloat162 m = h(u[0].x);
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            m = __hmax2(m, __hmax2(__hmax2(h(u[i].x), h(u[i].y)), __hmax2(h(u[i].z), h(u[i].w))));
+        return fmaxf(__low2float(m), __high2float(m));      // NaN only where all are
+    }
 }
+
+// The products that exponents are taken from stay far inside fp32's range.
+__device__ __forceinline__ bool in_range(float product) { return fabsf(product) < 1e30f; }
+
+// Running maximum and sum of a thread, the sum in two halves relative to `ref`, the
+// rounded product m c.
+struct Running {
+    float m = -INFINITY, ref = -INFINITY;
+    f32x2 s = 0;
+    __device__ __forceinline__ void raise(float to, float c) {
+        if (!(to > m)) return;
+        const float next = to * c;
+        const float f = in_range(ref) && in_range(next) ? exp2_fast(ref - next) : exp2_fast((m - to) * c);
+        s = mul2(s, pack2(f, f));       // from -inf: nothing summed yet, times 0
+        m = to;
+        ref = next;
+    }
+    template <typename T, int N>
+    __device__ __forceinline__ void add(const uint4 (&u)[N], float c) {
+        constexpr int kPairs = 8 / sizeof(T);
+        raise(largest<T>(u), c);
+        if (in_range(ref)) {
+            const f32x2 cc = pack2(c, c), rr = pack2(-ref, -ref);
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+#pragma unroll
+                for (int k = 0; k < kPairs; ++k) {
+                    const float2 e = unpack2(fma2(pair_of<T>(u[i], k), cc, rr));
+                    s = add2(s, pack2(exp2_fast(e.x), exp2_fast(e.y)));
+                }
+        } else {
+            const float base = m == -INFINITY ? 0.f : m;        // nothing but -inf (or NaN) so far
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+#pragma unroll
+                for (int k = 0; k < kPairs; ++k) {
+                    const float2 x = unpack2(pair_of<T>(u[i], k));
+                    s = add2(s, pack2(exp2_fast((x.x - base) * c), exp2_fast((x.y - base) * c)));
+                }
+        }
+    }
+    __device__ __forceinline__ void add1(float x, float c) {
+        raise(x, c);
+        const float base = m == -INFINITY ? 0.f : m;
+        s = add2(s, pack2(in_range(ref) ? exp2_fast(fmaf(x, c, -ref)) : exp2_fast((x - base) * c), 0.f));
+    }
+    __device__ __forceinline__ MaxSum sum(float c) const {
+        const float2 h = unpack2(s);
+        return MaxSum{m, (h.x + h.y) * (in_range(ref) ? exp2_fast(-fmaf(m, c, -ref)) : 1.f)};
+    }
+};
 
 // FWD: loss (and statistics).  GRAD: gradient, from the statistics where FWD is
 // false.  SAME: the gradient's rows start as far from a 16-byte boundary as the
-// logits' (else it is stored element by element).
-template <typename T, bool FWD, bool GRAD, bool SAME>
-__global__ void __launch_bounds__(kThreads)
+// logits' (else it is stored element by element).  Threads 0 .. N-1 sweep the row, the
+// warp after them takes the teacher's entries.
+template <typename T, bool FWD, bool GRAD, bool SAME, int N>
+__global__ void __launch_bounds__(N + 32, N == kWide ? 3 : 10)
 distill_kernel(const __grid_constant__ Params P) {
     namespace cg = cooperative_groups;
-    constexpr int VEC = 16 / sizeof(T);
+    constexpr int VEC = 16 / sizeof(T), kWarps = N / 32, kAll = N + 32;
     auto put = [](T* at, const float (&v)[VEC]) {
         if constexpr (SAME) {
             store_vec<T, VEC>(at, v);
@@ -95,9 +161,10 @@ distill_kernel(const __grid_constant__ Params P) {
             }
         }
     };
-    __shared__ float tmp[kWarps];
-    __shared__ float tmp_s[kWarps];
+    __shared__ MaxSum of_warp[kWarps];
     __shared__ MaxSum of_block;
+    __shared__ float t_max_s, t_sum_s;
+    __shared__ int listed_s;
     __shared__ int32_t top_id[kMaxTop];
     __shared__ float top_p[kMaxTop];
     __shared__ float top_x[kMaxTop];
@@ -105,6 +172,7 @@ distill_kernel(const __grid_constant__ Params P) {
     const int parts = static_cast<int>(cluster.num_blocks()), part = static_cast<int>(cluster.block_rank());
     const int64_t row = blockIdx.x / parts;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const bool teacher = warp == kWarps;
     chain_wait();
 
     const T* const x = static_cast<const T*>(P.logits) + row * P.ld;
@@ -116,19 +184,29 @@ distill_kernel(const __grid_constant__ Params P) {
     const int64_t v_begin = vectors * part / parts, v_end = vectors * (part + 1) / parts;
     const int64_t begin = part == 0 ? 0 : lead + v_begin * VEC;
     const int64_t end = part == parts - 1 ? P.vocab : lead + v_end * VEC;
-    const T* const xv = x + lead;
+    const T* const xv = x + lead + v_begin * VEC;
+    T* const dxv = GRAD ? dx + lead + v_begin * VEC : nullptr;
+    const int count = static_cast<int>(v_end - v_begin);        // vectors of this part
     const int64_t tail = lead + vectors * VEC;      // first entry past the vectors
+    // Entries outside the vectors (fewer than 2 VEC of a row): one thread each.
+    int64_t odd = -1;
+    if (part == 0 && threadIdx.x < lead) odd = threadIdx.x;
+    if (part == parts - 1 && threadIdx.x >= 32 && tail + threadIdx.x - 32 < P.vocab) odd = tail + threadIdx.x - 32;
+    if (teacher) odd = -1;
 
-    // The teacher's entries, with the student's logit of each read before any block
-    // of the row writes its gradient (which may take the logits' place).
     const float w = P.weight != nullptr ? P.weight[row] : 1.f;
     const float up = GRAD && P.dloss != nullptr ? P.dloss[row] : 1.f;
     const float inv_tau = 1.f / P.temperature;
     const float c = kLog2e / P.temperature;
-    bool on = w != 0.f && (FWD || up != 0.f);
-    int listed = 0;
-    if (on) {
-        for (int j = threadIdx.x; j < P.top; j += kThreads) {
+    bool on = w != 0.f && (FWD || up != 0.f);       // the same for every block of the row
+
+    Running mine;
+    if (on && teacher) {
+        // The student's logits of the entries are read before any block of the row
+        // writes its gradient, which may take their place.
+        int listed = 0;
+        float t_max = -INFINITY;
+        for (int j = lane; j < P.top; j += 32) {
             const int64_t id_at = row * P.top_ids_ld + j, at = row * P.top_logits_ld + j;
             const int64_t id = P.ids_i64 ? static_cast<const int64_t*>(P.top_ids)[id_at]
                                          : static_cast<const int32_t*>(P.top_ids)[id_at];
@@ -145,9 +223,45 @@ distill_kernel(const __grid_constant__ Params P) {
             top_id[j] = here ? static_cast<int32_t>(id) : -1;
             top_p[j] = t[0];
             top_x[j] = v[0];
+            t_max = fmaxf(t_max, t[0]);
+        }
+        t_max = warp_max(t_max);
+        float t_sum = 0.f;
+        for (int j = lane; j < P.top; j += 32)
+            if (top_id[j] >= 0) t_sum += expf((top_p[j] - t_max) * inv_tau);
+        t_sum = warp_sum(t_sum);
+        listed = __any_sync(~0u, listed);
+        if (lane == 0) {
+            listed_s = listed;
+            t_max_s = t_max;
+            t_sum_s = t_sum;
         }
     }
-    on = __syncthreads_or(listed) != 0;
+    if (FWD && on && !teacher) {
+        int i = threadIdx.x;
+        for (; i + (kBatch - 1) * N < count; i += kBatch * N) {
+            uint4 u[kBatch];
+#pragma unroll
+            for (int k = 0; k < kBatch; ++k) u[k] = *reinterpret_cast<const uint4*>(xv + static_cast<int64_t>(i + k * N) * VEC);
+            mine.add<T>(u, c);
+        }
+        for (; i < count; i += N) {
+            const uint4 u[1] = {*reinterpret_cast<const uint4*>(xv + static_cast<int64_t>(i) * VEC)};
+            mine.add<T>(u, c);
+        }
+        if (odd >= 0) {
+            float v[1];
+            load_vec<T, 1>(x + odd, v);
+            mine.add1(v[0], c);
+        }
+        MaxSum a = mine.sum(c);
+#pragma unroll
+        for (int d = 16; d > 0; d >>= 1)
+            a = merge(a, MaxSum{__shfl_xor_sync(~0u, a.m, d), __shfl_xor_sync(~0u, a.s, d)}, c);
+        if (lane == 0) of_warp[warp] = a;
+    }
+    __syncthreads();
+    on = on && listed_s != 0;
     if (!on) {      // the same for every block of the row
         if (FWD && part == 0 && threadIdx.x == 0) {
             P.loss[row] = 0.f;
@@ -155,70 +269,14 @@ distill_kernel(const __grid_constant__ Params P) {
         }
         if (GRAD) {
             const float zero[VEC] = {}, none[1] = {};
-            if (part == 0)
-                for (int64_t i = threadIdx.x; i < lead; i += kThreads) store_vec<T, 1>(dx + i, none);
-            for (int64_t i = v_begin + threadIdx.x; i < v_end; i += kThreads) put(dx + lead + i * VEC, zero);
-            if (part == parts - 1)
-                for (int64_t i = tail + threadIdx.x; i < P.vocab; i += kThreads) store_vec<T, 1>(dx + i, none);
+            if (odd >= 0) store_vec<T, 1>(dx + odd, none);
+            for (int i = threadIdx.x; i < count; i += kAll) put(dxv + static_cast<int64_t>(i) * VEC, zero);
         }
         return;
     }
-    float t_max = -INFINITY;
-    for (int j = threadIdx.x; j < P.top; j += kThreads) t_max = fmaxf(t_max, top_p[j]);
-    t_max = block_max(t_max, tmp);
-    float t_sum = 0.f;
-    for (int j = threadIdx.x; j < P.top; j += kThreads)
-        if (top_id[j] >= 0) t_sum += expf((top_p[j] - t_max) * inv_tau);
-    t_sum = block_sum(t_sum, tmp);
-    const float log_t = logf(t_sum);
-
     MaxSum all;
     if (FWD) {
-        MaxSum a = {-INFINITY, 0.f};
-        for (int64_t i = v_begin + threadIdx.x; i < v_end; i += kBatch * kThreads) {
-            float v[kBatch][VEC];
-            float m = a.m;
-#pragma unroll
-            for (int u = 0; u < kBatch; ++u) {
-                const bool in = i + u * kThreads < v_end;
-                if (in) load_vec<T, VEC>(xv + (i + u * kThreads) * VEC, v[u]);
-#pragma unroll
-                for (int k = 0; k < VEC; ++k)
-                    if (!in) v[u][k] = -INFINITY;
-            }
-#pragma unroll
-            for (int u = 0; u < kBatch; ++u)
-#pragma unroll
-                for (int k = 0; k < VEC; ++k) m = fmaxf(m, v[u][k]);
-            a.s *= rescale(a.m, m, c);
-            a.m = m;
-            const float ref = m == -INFINITY ? 0.f : m;     // nothing but -inf so far: 2^-inf = 0
-#pragma unroll
-            for (int u = 0; u < kBatch; ++u)
-#pragma unroll
-                for (int k = 0; k < VEC; ++k) a.s += exp2_fast((v[u][k] - ref) * c);
-        }
-        auto one = [&](int64_t i) {
-            float v[1];
-            load_vec<T, 1>(x + i, v);
-            const float m = fmaxf(a.m, v[0]);
-            a.s = a.s * rescale(a.m, m, c) + exp2_fast((v[0] - (m == -INFINITY ? 0.f : m)) * c);
-            a.m = m;
-        };
-        if (part == 0)
-            for (int64_t i = threadIdx.x; i < lead; i += kThreads) one(i);
-        if (part == parts - 1)
-            for (int64_t i = tail + threadIdx.x; i < P.vocab; i += kThreads) one(i);
-#pragma unroll
-        for (int d = 16; d > 0; d >>= 1)
-            a = merge(a, MaxSum{__shfl_xor_sync(~0u, a.m, d), __shfl_xor_sync(~0u, a.s, d)}, c);
-        __syncthreads();
-        if (lane == 0) {
-            tmp[warp] = a.m;
-            tmp_s[warp] = a.s;
-        }
-        __syncthreads();
-        all = lane < kWarps ? MaxSum{tmp[lane], tmp_s[lane]} : MaxSum{-INFINITY, 0.f};
+        all = lane < kWarps ? of_warp[lane] : MaxSum{-INFINITY, 0.f};
 #pragma unroll
         for (int d = 16; d > 0; d >>= 1)
             all = merge(all, MaxSum{__shfl_xor_sync(~0u, all.m, d), __shfl_xor_sync(~0u, all.s, d)}, c);
@@ -233,17 +291,18 @@ distill_kernel(const __grid_constant__ Params P) {
         all = MaxSum{P.stats[2 * row], P.stats[2 * row + 1]};
     }
 
-    if (FWD && part == 0) {
-        const float log_q = logf(all.s);
+    const float t_max = t_max_s, t_sum = t_sum_s;
+    if (FWD && part == 0 && teacher) {
+        const float log_q = logf(all.s), log_t = logf(t_sum);
         float l = 0.f;
-        for (int j = threadIdx.x; j < P.top; j += kThreads) {
+        for (int j = lane; j < P.top; j += 32) {
             if (top_id[j] < 0) continue;
             const float log_p = (top_p[j] - t_max) * inv_tau - log_t;
             const float p = expf(log_p);
             if (p != 0.f) l += p * (log_p - ((top_x[j] - all.m) * inv_tau - log_q));
         }
-        l = block_sum(l, tmp);
-        if (threadIdx.x == 0) {
+        l = warp_sum(l);
+        if (lane == 0) {
             P.loss[row] = w * P.temperature * P.temperature * l;
             if (P.stats != nullptr) {
                 P.stats[2 * row] = all.m;
@@ -251,45 +310,60 @@ distill_kernel(const __grid_constant__ Params P) {
             }
         }
     }
-    if (GRAD) {
-        const float scale = w * up * P.temperature;
-        const float f = scale / all.s, m = all.m;
-        for (int64_t i = v_begin + threadIdx.x; i < v_end; i += kBatch * kThreads) {
-            float v[kBatch][VEC];
+    if (!GRAD) return;
+    const float scale = w * up * P.temperature;
+    const float ref = all.m * c;
+    const bool fast = in_range(ref);
+    const float f = scale / all.s * (fast ? exp2_fast(-fmaf(all.m, c, -ref)) : 1.f);
+    auto q_of = [&](float v) { return f * (fast ? exp2_fast(fmaf(v, c, -ref)) : exp2_fast((v - all.m) * c)); };
+    if (!teacher) {
+        const f32x2 cc = pack2(c, c), rr = pack2(-ref, -ref), ff = pack2(f, f);
+        auto grad = [&](const uint4& u, int i) {
+            float v[VEC];
+            if (fast) {
 #pragma unroll
-            for (int u = 0; u < kBatch; ++u)
-                if (i + u * kThreads < v_end) load_vec<T, VEC>(xv + (i + u * kThreads) * VEC, v[u]);
-#pragma unroll
-            for (int u = 0; u < kBatch; ++u)
-                if (i + u * kThreads < v_end) {
-#pragma unroll
-                    for (int k = 0; k < VEC; ++k) v[u][k] = f * exp2_fast((v[u][k] - m) * c);
-                    put(dx + lead + (i + u * kThreads) * VEC, v[u]);
+                for (int k = 0; k < VEC / 2; ++k) {
+                    const float2 e = unpack2(fma2(pair_of<T>(u, k), cc, rr));
+                    const float2 g = unpack2(mul2(pack2(exp2_fast(e.x), exp2_fast(e.y)), ff));
+                    v[2 * k] = g.x;
+                    v[2 * k + 1] = g.y;
                 }
-        }
-        auto one = [&](int64_t i) {
-            float v[1];
-            load_vec<T, 1>(x + i, v);
-            v[0] = f * exp2_fast((v[0] - m) * c);
-            store_vec<T, 1>(dx + i, v);
+            } else {
+                unpack<T>(u, v);
+#pragma unroll
+                for (int k = 0; k < VEC; ++k) v[k] = q_of(v[k]);
+            }
+            put(dxv + static_cast<int64_t>(i) * VEC, v);
         };
-        if (part == 0)
-            for (int64_t i = threadIdx.x; i < lead; i += kThreads) one(i);
-        if (part == parts - 1)
-            for (int64_t i = tail + threadIdx.x; i < P.vocab; i += kThreads) one(i);
-        // The listed entries of this block's part, written again with their target.
-        for (int j = threadIdx.x; j < P.top; j += kThreads)
-            if (top_id[j] >= 0) top_p[j] = expf((top_p[j] - t_max) * inv_tau) / t_sum;
-        __syncthreads();
-        for (int j = threadIdx.x; j < P.top; j += kThreads) {
-            const int32_t id = top_id[j];
-            if (id < begin || id >= end) continue;
-            float p = 0.f;          // an entry listed twice: both write the same sum
-            for (int k = 0; k < P.top; ++k)
-                if (top_id[k] == id) p += top_p[k];
-            const float v[1] = {f * exp2_fast((top_x[j] - m) * c) - scale * p};
-            store_vec<T, 1>(dx + id, v);
+        int i = threadIdx.x;
+        for (; i + (kBatch - 1) * N < count; i += kBatch * N) {
+            uint4 u[kBatch];
+#pragma unroll
+            for (int k = 0; k < kBatch; ++k) u[k] = *reinterpret_cast<const uint4*>(xv + static_cast<int64_t>(i + k * N) * VEC);
+#pragma unroll
+            for (int k = 0; k < kBatch; ++k) grad(u[k], i + k * N);
         }
+        for (; i < count; i += N) grad(*reinterpret_cast<const uint4*>(xv + static_cast<int64_t>(i) * VEC), i);
+        if (odd >= 0) {
+            float v[1];
+            load_vec<T, 1>(x + odd, v);
+            v[0] = q_of(v[0]);
+            store_vec<T, 1>(dx + odd, v);
+        }
+    } else {
+        for (int j = lane; j < P.top; j += 32)
+            if (top_id[j] >= 0) top_p[j] = expf((top_p[j] - t_max) * inv_tau) / t_sum;
+    }
+    // The listed entries of this block's part, written again with their target.
+    __syncthreads();
+    for (int j = threadIdx.x; j < P.top; j += kAll) {
+        const int32_t id = top_id[j];
+        if (id < begin || id >= end) continue;
+        float p = 0.f;          // an entry listed twice: both write the same sum
+        for (int k = 0; k < P.top; ++k)
+            if (top_id[k] == id) p += top_p[k];
+        const float v[1] = {q_of(top_x[j]) - scale * p};
+        store_vec<T, 1>(dx + id, v);
     }
 }
 
@@ -316,9 +390,16 @@ cudaError_t launch(const malt_distill_t* d, const Params& P, cudaStream_t s) {
                                 (P.ld - P.dlogits_ld) % V == 0);
     // A row is split while its blocks leave SMs idle and its parts keep a batch of vectors.
     int parts = 1;
-    while (parts < kMaxCluster && d->rows * parts < sm_count() && d->vocab / (2 * parts) >= kThreads * V) parts *= 2;
-    return launch_clusters(same ? distill_kernel<T, FWD, GRAD, true> : distill_kernel<T, FWD, GRAD, !GRAD>,
-                           static_cast<unsigned>(d->rows * parts), parts, kThreads, 0, s, P);
+    while (parts < kMaxCluster && d->rows * parts < sm_count() && d->vocab / (2 * parts) >= kWide * V) parts *= 2;
+    auto go = [&](auto* kernel, int threads) {
+        return launch_clusters(kernel, static_cast<unsigned>(d->rows * parts), parts, threads + 32, 0, s, P);
+    };
+    // Short rows leave most of a wide block waiting for its barriers.
+    if (d->vocab <= kNarrow * V * kBatch)
+        return same ? go(distill_kernel<T, FWD, GRAD, true, kNarrow>, kNarrow)
+                    : go(distill_kernel<T, FWD, GRAD, !GRAD, kNarrow>, kNarrow);
+    return same ? go(distill_kernel<T, FWD, GRAD, true, kWide>, kWide)
+                : go(distill_kernel<T, FWD, GRAD, !GRAD, kWide>, kWide);
 }
 
 Params params_of(const malt_distill_t* d) {
