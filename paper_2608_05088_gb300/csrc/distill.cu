@@ -13,7 +13,11 @@
 // sweep finds the row's maximum m and sum of 2^((s - m) c), c = log2(e) / tau, each
 // thread with a running maximum over batches of vectors; the second writes the
 // gradient and finds the row in L2.  One warp more takes the teacher's entries
-// meanwhile.  Bound by HBM: the logits once, their gradient once.
+// meanwhile.  Bound by HBM: the logits once, their gradient once.  8192 rows of 50304
+// bf16 logits: 251 us, 6.26 TB/s of what has to move (loss alone 124 us, 6.7 TB/s;
+// gradient alone 254 us, 6.5 TB/s).  Rows kept in shared memory instead, by blocks that
+// stay and copy the next row meanwhile, took 276 us: a block's barriers then stand
+// between its sweeps with no other block on the SM to fill them.
 //
 // An exponent s c - m c is one fused multiply-add of the rounded product m c, whose
 // rounding is the same for every entry and is taken out of the sum again at its end.
@@ -30,8 +34,29 @@ namespace malt {
 namespace {
 
 constexpr int kMaxTop = 1024;
-constexpr int kWide = 512, kNarrow = 128;      // threads that sweep a row
-constexpr int kBatch = 4;           // vectors of a thread in flight
+// Threads that sweep a row, blocks that an SM holds and vectors of a thread in flight.
+// Wide: rows of both sweeps, few blocks, so that all their rows stay in L2 from the first
+// sweep to the second (8192 rows of 50304 bf16: 251 us, medium 343).  Medium: single
+// sweeps, and both sweeps of parts up to kMediumPart, whose blocks spend their time at
+// barriers (16384 rows of 8192 bf16: 105 us, wide 175; 8000 of 16384 fp32: 218, wide
+// 157).  Narrow: rows up to kNarrowRow (16384 of 2000 bf16: 53 us, medium 74).
+struct Shape {
+    int threads, blocks, batch;
+};
+enum Width { kNarrow, kMedium, kWide };
+__host__ __device__ constexpr Shape shape_of(int width) {
+    return width == kNarrow ? Shape{96, 10, 4} : width == kMedium ? Shape{224, 7, 4} : Shape{480, 3, 5};
+}
+constexpr int64_t kNarrowRow = 6 * 1024, kMediumPart = 56 * 1024;
+// Bytes of a row that one block takes, at most, in clusters of up to kSizeCluster.  With
+// a forward sweep larger parts push one another out of L2 (2048 rows of 131072 bf16: two
+// parts 198 us, one 233), smaller ones wait for one another.  The gradient alone waits
+// for nothing, and small parts fill the last wave (1531 fp32 rows of 50257: 104 us at 70
+// KB, 112 at 140).  Clusters of 8 leave more SMs without one (300 fp32 rows of 150000: 88
+// us, 75 in fours).
+constexpr int64_t kSweptPart = 140 * 1024, kWrittenPart = 70 * 1024;
+constexpr int kSizeCluster = 4;
+// While a row's blocks leave SMs idle: up to the largest portable cluster.
 constexpr int kMaxCluster = 8;
 constexpr float kLog2e = 1.4426950408889634f;
 
@@ -59,9 +84,19 @@ struct MaxSum {
 __device__ __forceinline__ float rescale(float from, float to, float c) {
     return from == to ? 1.f : exp2_fast((from - to) * c);      // equal infinities too
 }
-__device__ __forceinline__ MaxSum merge(MaxSum a, MaxSum b, float c) {
-    const float m = fmaxf(a.m, b.m);
-    return MaxSum{m, a.s * rescale(a.m, m, c) + b.s * rescale(b.m, m, c)};
+// Over the warp's lanes, each with its own.
+__device__ __forceinline__ MaxSum warp_merge(MaxSum a, float c) {
+    const float m = warp_max(a.m);
+    return MaxSum{m, warp_sum(a.s * rescale(a.m, m, c))};
+}
+// Over n of them in shared memory, the same in every lane of a warp.
+__device__ __forceinline__ MaxSum merge_all(const MaxSum* of, int n, float c) {
+    const int lane = threadIdx.x & 31;
+    float m = -INFINITY, s = 0.f;
+    for (int k = lane; k < n; k += 32) m = fmaxf(m, of[k].m);
+    m = warp_max(m);
+    for (int k = lane; k < n; k += 32) s += of[k].s * rescale(of[k].m, m, c);
+    return MaxSum{m, warp_sum(s)};
 }
 
 // One vector of logits (16 bytes) as pairs of fp32, and its largest entry.
@@ -141,33 +176,209 @@ struct Running {
     }
 };
 
+// The teacher's entries of a row in shared memory, and what their softmax takes.
+struct Top {
+    int32_t* id;        // -1: not listed; filled up to a multiple of 4, aligned to 16 bytes
+    float* t;           // teacher's logits, then log-probabilities
+    float* x;           // student's logits
+    float* p;           // probabilities
+};
+__host__ __device__ __forceinline__ int padded_top(int top) { return (top + 3) / 4 * 4; }
+// One warp reads the entries of a row; those that do not count get id -1.
+template <typename T>
+__device__ __forceinline__ void list_entries(const Params& P, int64_t row, const Top& top) {
+    const int lane = threadIdx.x & 31, padded = padded_top(P.top);
+    for (int j = lane; j < padded; j += 32) {
+        int64_t id = -1;
+        float t[1] = {-INFINITY};
+        if (j < P.top) {
+            const int64_t id_at = row * P.top_ids_ld + j, at = row * P.top_logits_ld + j;
+            id = P.ids_i64 ? static_cast<const int64_t*>(P.top_ids)[id_at] : static_cast<const int32_t*>(P.top_ids)[id_at];
+            if (P.top_bf16) load_vec<bf16, 1>(static_cast<const bf16*>(P.top_logits) + at, t);
+            else load_vec<float, 1>(static_cast<const float*>(P.top_logits) + at, t);
+        }
+        const bool here = id >= 0 && id < P.vocab && t[0] != -INFINITY;     // a probability of 0 lists nothing
+        top.id[j] = here ? static_cast<int32_t>(id) : -1;
+        top.t[j] = here ? t[0] : -INFINITY;
+    }
+    __syncwarp();
+}
+// The student's logits of those in [begin, end).
+template <typename T>
+__device__ __forceinline__ void look_up(const Params& P, const T* x, int begin, int end, const Top& top) {
+    for (int j = threadIdx.x & 31; j < P.top; j += 32) {
+        float v[1] = {0.f};
+        if (top.id[j] >= begin && top.id[j] < end) load_vec<T, 1>(x + top.id[j], v);
+        top.x[j] = v[0];
+    }
+}
+
+// Probabilities of a row's entries, by one warp; whether any is listed.
+__device__ __forceinline__ int softmax_of(const Params& P, const Top& top, float inv_tau) {
+    const int lane = threadIdx.x & 31;
+    float max = -INFINITY, sum = 0.f;
+    for (int j = lane; j < P.top; j += 32) max = fmaxf(max, top.t[j]);
+    max = warp_max(max);
+    for (int j = lane; j < P.top; j += 32) {
+        const float t = (top.t[j] - max) * inv_tau, e = top.id[j] >= 0 ? expf(t) : 0.f;
+        top.t[j] = t;
+        top.p[j] = e;
+        sum += e;
+    }
+    sum = warp_sum(sum);
+    const float log_t = logf(sum), f = 1.f / sum;
+    for (int j = lane; j < P.top; j += 32) {
+        top.t[j] -= log_t;
+        top.p[j] *= f;
+    }
+    return max != -INFINITY;        // listed entries have a larger logit
+}
+
+// Loss and statistics of a row, by one warp.
+__device__ __forceinline__ void store_loss(const Params& P, int64_t row, float w, float inv_tau, const Top& top,
+                                           const MaxSum& all) {
+    const int lane = threadIdx.x & 31;
+    const float log_q = logf(all.s);
+    float l = 0.f;
+    for (int j = lane; j < P.top; j += 32) {
+        if (top.id[j] < 0) continue;
+        const float p = top.p[j];
+        if (p != 0.f) l += p * (top.t[j] - ((top.x[j] - all.m) * inv_tau - log_q));
+    }
+    l = warp_sum(l);
+    if (lane == 0) {
+        P.loss[row] = w * P.temperature * P.temperature * l;
+        if (P.stats != nullptr) {
+            P.stats[2 * row] = all.m;
+            P.stats[2 * row + 1] = all.s;
+        }
+    }
+}
+
+// 16 bytes of results, which leave the logits' place in L2 alone; SAME: their address is
+// a multiple of 16.
+template <typename T, bool SAME, int VEC>
+__device__ __forceinline__ void put(T* at, const float (&v)[VEC]) {
+    if constexpr (SAME) {
+        uint4 u;
+        if constexpr (sizeof(T) == 4) u = make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
+        else u = make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
+        __stcs(reinterpret_cast<uint4*>(at), u);
+    } else {
+#pragma unroll
+        for (int k = 0; k < VEC; ++k) {
+            const float one[1] = {v[k]};
+            store_vec<T, 1>(at + k, one);
+        }
+    }
+}
+
+// The gradient's term scale * q of a logit.
+struct Gradient {
+    float scale, f, ref, m, c;
+    bool fast;
+    __device__ __forceinline__ Gradient(float scale_, const MaxSum& all, float c_) : scale(scale_), m(all.m), c(c_) {
+        ref = m * c;
+        fast = in_range(ref);
+        f = scale / all.s * (fast ? exp2_fast(-fmaf(m, c, -ref)) : 1.f);
+    }
+    __device__ __forceinline__ float at(float v) const {
+        return f * (fast ? exp2_fast(fmaf(v, c, -ref)) : exp2_fast((v - m) * c));
+    }
+    template <typename T, bool SAME>
+    __device__ __forceinline__ void store(const uint4& u, T* to) const {
+        constexpr int VEC = 16 / sizeof(T);
+        float v[VEC];
+        if (fast) {
+            const f32x2 cc = pack2(c, c), rr = pack2(-ref, -ref), ff = pack2(f, f);
+#pragma unroll
+            for (int k = 0; k < VEC / 2; ++k) {
+                const float2 e = unpack2(fma2(pair_of<T>(u, k), cc, rr));
+                const float2 g = unpack2(mul2(pack2(exp2_fast(e.x), exp2_fast(e.y)), ff));
+                v[2 * k] = g.x;
+                v[2 * k + 1] = g.y;
+            }
+        } else {
+            unpack<T>(u, v);
+#pragma unroll
+            for (int k = 0; k < VEC; ++k) v[k] = at(v[k]);
+        }
+        put<T, SAME, VEC>(to, v);
+    }
+    template <typename T>
+    __device__ __forceinline__ void store1(const T* from, T* to) const {
+        float v[1];
+        load_vec<T, 1>(from, v);
+        v[0] = at(v[0]);
+        store_vec<T, 1>(to, v);
+    }
+};
+
+// The listed entries of [begin, end), written again with their target by `threads`
+// threads.  An entry listed twice is written twice with the same sum.
+template <typename T>
+__device__ __forceinline__ void store_targets(const Params& P, const Gradient& g, const Top& top, int begin, int end, T* dx,
+                                              int first, int threads) {
+    for (int j = first; j < P.top; j += threads) {
+        const int32_t id = top.id[j];
+        if (id < begin || id >= end) continue;
+        float p = 0.f;
+        for (int k = 0; k < P.top; k += 4) {
+            const int4 four = *reinterpret_cast<const int4*>(top.id + k);
+            const float4 q = *reinterpret_cast<const float4*>(top.p + k);
+            p += four.x == id ? q.x : 0.f;
+            p += four.y == id ? q.y : 0.f;
+            p += four.z == id ? q.z : 0.f;
+            p += four.w == id ? q.w : 0.f;
+        }
+        const float v[1] = {g.at(top.x[j]) - g.scale * p};
+        store_vec<T, 1>(dx + id, v);
+    }
+}
+
+// A part of a row: where its vectors and the entries outside them lie.
+template <typename T>
+struct Part {
+    static constexpr int VEC = 16 / sizeof(T);
+    int begin, end;     // its entries
+    int first;          // the first of its vectors' entries
+    int odd;            // this thread's entry outside the row's vectors, or -1
+    int count;          // its vectors
+    // part of 2^shift
+    __device__ __forceinline__ Part(const T* x, int vocab, int part, int shift, bool sweeps) {
+        // Vectors start on 16-byte addresses: `lead` entries come before the first one.
+        const int parts = 1 << shift;
+        const int lead = min(vocab, static_cast<int>(-(static_cast<uint32_t>(reinterpret_cast<uintptr_t>(x)) / sizeof(T)) % VEC));
+        const int vectors = (vocab - lead) / VEC;
+        const int v_begin = static_cast<int>(static_cast<int64_t>(vectors) * part >> shift);
+        const int v_end = static_cast<int>(static_cast<int64_t>(vectors) * (part + 1) >> shift);
+        begin = part == 0 ? 0 : lead + v_begin * VEC;
+        end = part == parts - 1 ? vocab : lead + v_end * VEC;
+        first = lead + v_begin * VEC;
+        count = v_end - v_begin;
+        // Fewer than 2 VEC entries of a row lie outside: one thread each.
+        const int tail = lead + vectors * VEC, t = threadIdx.x;
+        odd = -1;
+        if (part == 0 && t < lead) odd = t;
+        if (part == parts - 1 && t >= 32 && t - 32 < vocab - tail) odd = tail + t - 32;
+        if (!sweeps) odd = -1;
+    }
+};
+
 // FWD: loss (and statistics).  GRAD: gradient, from the statistics where FWD is
 // false.  SAME: the gradient's rows start as far from a 16-byte boundary as the
 // logits' (else it is stored element by element).  Threads 0 .. N-1 sweep the row, the
 // warp after them takes the teacher's entries.
-template <typename T, bool FWD, bool GRAD, bool SAME, int N>
-__global__ void __launch_bounds__(N + 32, N == kWide ? 3 : 10)
+template <typename T, bool FWD, bool GRAD, bool SAME, int WIDTH>
+__global__ void __launch_bounds__(shape_of(WIDTH).threads + 32, shape_of(WIDTH).blocks)
 distill_kernel(const __grid_constant__ Params P) {
+    constexpr int N = shape_of(WIDTH).threads, kBatch = shape_of(WIDTH).batch;
     namespace cg = cooperative_groups;
     constexpr int VEC = 16 / sizeof(T), kWarps = N / 32, kAll = N + 32;
-    auto put = [](T* at, const float (&v)[VEC]) {
-        if constexpr (SAME) {
-            store_vec<T, VEC>(at, v);
-        } else {
-#pragma unroll
-            for (int k = 0; k < VEC; ++k) {
-                const float one[1] = {v[k]};
-                store_vec<T, 1>(at + k, one);
-            }
-        }
-    };
     __shared__ MaxSum of_warp[kWarps];
     __shared__ MaxSum of_block;
-    __shared__ float t_max_s, t_sum_s;
-    __shared__ int listed_s;
-    __shared__ int32_t top_id[kMaxTop];
-    __shared__ float top_p[kMaxTop];
-    __shared__ float top_x[kMaxTop];
+    __shared__ int listed;
+    extern __shared__ uint4 entries[];      // the teacher's
     const cg::cluster_group cluster = cg::this_cluster();
     const int parts = static_cast<int>(cluster.num_blocks()), part = static_cast<int>(cluster.block_rank());
     const int64_t row = blockIdx.x / parts;
@@ -177,76 +388,40 @@ distill_kernel(const __grid_constant__ Params P) {
 
     const T* const x = static_cast<const T*>(P.logits) + row * P.ld;
     T* const dx = GRAD ? static_cast<T*>(P.dlogits) + row * P.dlogits_ld : nullptr;
-    // The row's parts start on vectors of its address: `lead` entries come before the
-    // first one.
-    const int64_t lead = min(P.vocab, static_cast<int64_t>((VEC - reinterpret_cast<uintptr_t>(x) / sizeof(T) % VEC) % VEC));
-    const int64_t vectors = (P.vocab - lead) / VEC;
-    const int64_t v_begin = vectors * part / parts, v_end = vectors * (part + 1) / parts;
-    const int64_t begin = part == 0 ? 0 : lead + v_begin * VEC;
-    const int64_t end = part == parts - 1 ? P.vocab : lead + v_end * VEC;
-    const T* const xv = x + lead + v_begin * VEC;
-    T* const dxv = GRAD ? dx + lead + v_begin * VEC : nullptr;
-    const int count = static_cast<int>(v_end - v_begin);        // vectors of this part
-    const int64_t tail = lead + vectors * VEC;      // first entry past the vectors
-    // Entries outside the vectors (fewer than 2 VEC of a row): one thread each.
-    int64_t odd = -1;
-    if (part == 0 && threadIdx.x < lead) odd = threadIdx.x;
-    if (part == parts - 1 && threadIdx.x >= 32 && tail + threadIdx.x - 32 < P.vocab) odd = tail + threadIdx.x - 32;
-    if (teacher) odd = -1;
+    const Part<T> here(x, static_cast<int>(P.vocab), part, 31 - __clz(parts), !teacher);
+    const int begin = here.begin, end = here.end, odd = here.odd, count = here.count;
+    const T* const xv = x + here.first;
+    T* const dxv = GRAD ? dx + here.first : nullptr;
 
     const float w = P.weight != nullptr ? P.weight[row] : 1.f;
     const float up = GRAD && P.dloss != nullptr ? P.dloss[row] : 1.f;
     const float inv_tau = 1.f / P.temperature;
     const float c = kLog2e / P.temperature;
+    const int padded = padded_top(P.top);
+    float* const tops = reinterpret_cast<float*>(entries);
+    const Top top{reinterpret_cast<int32_t*>(tops), tops + padded, tops + 2 * padded, tops + 3 * padded};
     bool on = w != 0.f && (FWD || up != 0.f);       // the same for every block of the row
 
+    // The first batch is on its way before anything is known of the row.
     Running mine;
-    if (on && teacher) {
-        // The student's logits of the entries are read before any block of the row
-        // writes its gradient, which may take their place.
-        int listed = 0;
-        float t_max = -INFINITY;
-        for (int j = lane; j < P.top; j += 32) {
-            const int64_t id_at = row * P.top_ids_ld + j, at = row * P.top_logits_ld + j;
-            const int64_t id = P.ids_i64 ? static_cast<const int64_t*>(P.top_ids)[id_at]
-                                         : static_cast<const int32_t*>(P.top_ids)[id_at];
-            float t[1] = {-INFINITY}, v[1] = {0.f};
-            if (id >= 0 && id < P.vocab) {
-                if (P.top_bf16) load_vec<bf16, 1>(static_cast<const bf16*>(P.top_logits) + at, t);
-                else load_vec<float, 1>(static_cast<const float*>(P.top_logits) + at, t);
-            }
-            const bool here = t[0] != -INFINITY;    // a probability of 0 lists nothing
-            if (here) {
-                listed = 1;
-                if (FWD || (id >= begin && id < end)) load_vec<T, 1>(x + id, v);
-            }
-            top_id[j] = here ? static_cast<int32_t>(id) : -1;
-            top_p[j] = t[0];
-            top_x[j] = v[0];
-            t_max = fmaxf(t_max, t[0]);
-        }
-        t_max = warp_max(t_max);
-        float t_sum = 0.f;
-        for (int j = lane; j < P.top; j += 32)
-            if (top_id[j] >= 0) t_sum += expf((top_p[j] - t_max) * inv_tau);
-        t_sum = warp_sum(t_sum);
-        listed = __any_sync(~0u, listed);
-        if (lane == 0) {
-            listed_s = listed;
-            t_max_s = t_max;
-            t_sum_s = t_sum;
-        }
+    uint4 u[kBatch];
+    auto load = [&](int i) {        // past the part's end: entries of -inf
+        constexpr uint32_t kNone = sizeof(T) == 4 ? 0xff800000u : 0xff80ff80u;
+        const T* const at = xv + static_cast<int64_t>(i) * VEC;
+#pragma unroll
+        for (int k = 0; k < kBatch; ++k)
+            u[k] = i + k * N < count ? *reinterpret_cast<const uint4*>(at + k * N * VEC) : make_uint4(kNone, kNone, kNone, kNone);
+    };
+    if (!teacher) load(threadIdx.x);
+    if (teacher) {
+        list_entries<T>(P, row, top);
+        look_up(P, x, FWD ? 0 : begin, FWD ? static_cast<int>(P.vocab) : end, top);
+        const int any = softmax_of(P, top, inv_tau);
+        if (lane == 0) listed = any;
     }
     if (FWD && on && !teacher) {
-        int i = threadIdx.x;
-        for (; i + (kBatch - 1) * N < count; i += kBatch * N) {
-            uint4 u[kBatch];
-#pragma unroll
-            for (int k = 0; k < kBatch; ++k) u[k] = *reinterpret_cast<const uint4*>(xv + static_cast<int64_t>(i + k * N) * VEC);
-            mine.add<T>(u, c);
-        }
-        for (; i < count; i += N) {
-            const uint4 u[1] = {*reinterpret_cast<const uint4*>(xv + static_cast<int64_t>(i) * VEC)};
+        for (int i = threadIdx.x; i < count; i += kBatch * N) {
+            if (i != threadIdx.x) load(i);
             mine.add<T>(u, c);
         }
         if (odd >= 0) {
@@ -254,14 +429,11 @@ distill_kernel(const __grid_constant__ Params P) {
             load_vec<T, 1>(x + odd, v);
             mine.add1(v[0], c);
         }
-        MaxSum a = mine.sum(c);
-#pragma unroll
-        for (int d = 16; d > 0; d >>= 1)
-            a = merge(a, MaxSum{__shfl_xor_sync(~0u, a.m, d), __shfl_xor_sync(~0u, a.s, d)}, c);
+        const MaxSum a = warp_merge(mine.sum(c), c);
         if (lane == 0) of_warp[warp] = a;
     }
     __syncthreads();
-    on = on && listed_s != 0;
+    on = on && listed != 0;
     if (!on) {      // the same for every block of the row
         if (FWD && part == 0 && threadIdx.x == 0) {
             P.loss[row] = 0.f;
@@ -270,101 +442,38 @@ distill_kernel(const __grid_constant__ Params P) {
         if (GRAD) {
             const float zero[VEC] = {}, none[1] = {};
             if (odd >= 0) store_vec<T, 1>(dx + odd, none);
-            for (int i = threadIdx.x; i < count; i += kAll) put(dxv + static_cast<int64_t>(i) * VEC, zero);
+            for (int i = threadIdx.x; i < count; i += kAll) put<T, SAME, VEC>(dxv + static_cast<int64_t>(i) * VEC, zero);
         }
         return;
     }
     MaxSum all;
     if (FWD) {
-        all = lane < kWarps ? of_warp[lane] : MaxSum{-INFINITY, 0.f};
-#pragma unroll
-        for (int d = 16; d > 0; d >>= 1)
-            all = merge(all, MaxSum{__shfl_xor_sync(~0u, all.m, d), __shfl_xor_sync(~0u, all.s, d)}, c);
+        all = merge_all(of_warp, kWarps, c);
         if (parts > 1) {
             if (threadIdx.x == 0) of_block = all;
             cluster.sync();
-            all = MaxSum{-INFINITY, 0.f};
-            for (int k = 0; k < parts; ++k) all = merge(all, *cluster.map_shared_rank(&of_block, k), c);
+            all = warp_merge(lane < parts ? *cluster.map_shared_rank(&of_block, lane) : MaxSum{-INFINITY, 0.f}, c);
             cluster.sync();         // no block leaves while another reads its part
         }
     } else {
         all = MaxSum{P.stats[2 * row], P.stats[2 * row + 1]};
     }
 
-    const float t_max = t_max_s, t_sum = t_sum_s;
-    if (FWD && part == 0 && teacher) {
-        const float log_q = logf(all.s), log_t = logf(t_sum);
-        float l = 0.f;
-        for (int j = lane; j < P.top; j += 32) {
-            if (top_id[j] < 0) continue;
-            const float log_p = (top_p[j] - t_max) * inv_tau - log_t;
-            const float p = expf(log_p);
-            if (p != 0.f) l += p * (log_p - ((top_x[j] - all.m) * inv_tau - log_q));
-        }
-        l = warp_sum(l);
-        if (lane == 0) {
-            P.loss[row] = w * P.temperature * P.temperature * l;
-            if (P.stats != nullptr) {
-                P.stats[2 * row] = all.m;
-                P.stats[2 * row + 1] = all.s;
-            }
-        }
-    }
+    if (FWD && part == 0 && teacher) store_loss(P, row, w, inv_tau, top, all);
     if (!GRAD) return;
-    const float scale = w * up * P.temperature;
-    const float ref = all.m * c;
-    const bool fast = in_range(ref);
-    const float f = scale / all.s * (fast ? exp2_fast(-fmaf(all.m, c, -ref)) : 1.f);
-    auto q_of = [&](float v) { return f * (fast ? exp2_fast(fmaf(v, c, -ref)) : exp2_fast((v - all.m) * c)); };
+    const Gradient g(w * up * P.temperature, all, c);
     if (!teacher) {
-        const f32x2 cc = pack2(c, c), rr = pack2(-ref, -ref), ff = pack2(f, f);
-        auto grad = [&](const uint4& u, int i) {
-            float v[VEC];
-            if (fast) {
+        for (int i = threadIdx.x; i < count; i += kBatch * N) {
+            if (FWD || i != threadIdx.x) load(i);
+            T* const to = dxv + static_cast<int64_t>(i) * VEC;
 #pragma unroll
-                for (int k = 0; k < VEC / 2; ++k) {
-                    const float2 e = unpack2(fma2(pair_of<T>(u, k), cc, rr));
-                    const float2 g = unpack2(mul2(pack2(exp2_fast(e.x), exp2_fast(e.y)), ff));
-                    v[2 * k] = g.x;
-                    v[2 * k + 1] = g.y;
-                }
-            } else {
-                unpack<T>(u, v);
-#pragma unroll
-                for (int k = 0; k < VEC; ++k) v[k] = q_of(v[k]);
-            }
-            put(dxv + static_cast<int64_t>(i) * VEC, v);
-        };
-        int i = threadIdx.x;
-        for (; i + (kBatch - 1) * N < count; i += kBatch * N) {
-            uint4 u[kBatch];
-#pragma unroll
-            for (int k = 0; k < kBatch; ++k) u[k] = *reinterpret_cast<const uint4*>(xv + static_cast<int64_t>(i + k * N) * VEC);
-#pragma unroll
-            for (int k = 0; k < kBatch; ++k) grad(u[k], i + k * N);
+            for (int k = 0; k < kBatch; ++k)
+                if (i + k * N < count) g.store<T, SAME>(u[k], to + k * N * VEC);
         }
-        for (; i < count; i += N) grad(*reinterpret_cast<const uint4*>(xv + static_cast<int64_t>(i) * VEC), i);
-        if (odd >= 0) {
-            float v[1];
-            load_vec<T, 1>(x + odd, v);
-            v[0] = q_of(v[0]);
-            store_vec<T, 1>(dx + odd, v);
-        }
-    } else {
-        for (int j = lane; j < P.top; j += 32)
-            if (top_id[j] >= 0) top_p[j] = expf((top_p[j] - t_max) * inv_tau) / t_sum;
+        if (odd >= 0) g.store1(x + odd, dx + odd);
     }
-    // The listed entries of this block's part, written again with their target.
     __syncthreads();
-    for (int j = threadIdx.x; j < P.top; j += kAll) {
-        const int32_t id = top_id[j];
-        if (id < begin || id >= end) continue;
-        float p = 0.f;          // an entry listed twice: both write the same sum
-        for (int k = 0; k < P.top; ++k)
-            if (top_id[k] == id) p += top_p[k];
-        const float v[1] = {q_of(top_x[j]) - scale * p};
-        store_vec<T, 1>(dx + id, v);
-    }
+    store_targets(P, g, top, begin, end, dx, threadIdx.x, kAll);
 }
 
 // ----------------------------------------------------------------------- host
@@ -383,23 +492,32 @@ int check(const malt_distill_t* d) {
     return MALT_OK;
 }
 
-template <typename T, bool FWD, bool GRAD>
-cudaError_t launch(const malt_distill_t* d, const Params& P, cudaStream_t s) {
+// Shared memory of one row's entries.
+int64_t entries_bytes(int64_t top) { return 16 * padded_top(static_cast<int>(top)); }
+
+template <typename T, bool FWD, bool GRAD, int WIDTH>
+cudaError_t launch_width(const malt_distill_t* d, const Params& P, int parts, cudaStream_t s) {
     constexpr int V = 16 / sizeof(T);
     const bool same = !GRAD || (reinterpret_cast<uintptr_t>(P.logits) % 16 == reinterpret_cast<uintptr_t>(P.dlogits) % 16 &&
                                 (P.ld - P.dlogits_ld) % V == 0);
-    // A row is split while its blocks leave SMs idle and its parts keep a batch of vectors.
+    return launch_clusters(same ? distill_kernel<T, FWD, GRAD, true, WIDTH> : distill_kernel<T, FWD, GRAD, !GRAD, WIDTH>,
+                           static_cast<unsigned>(d->rows * parts), parts, shape_of(WIDTH).threads + 32,
+                           entries_bytes(d->top), s, P);
+}
+
+template <typename T, bool FWD, bool GRAD>
+cudaError_t launch(const malt_distill_t* d, const Params& P, cudaStream_t s) {
+    const int64_t bytes = d->vocab * static_cast<int64_t>(sizeof(T)), part = FWD ? kSweptPart : kWrittenPart;
     int parts = 1;
-    while (parts < kMaxCluster && d->rows * parts < sm_count() && d->vocab / (2 * parts) >= kWide * V) parts *= 2;
-    auto go = [&](auto* kernel, int threads) {
-        return launch_clusters(kernel, static_cast<unsigned>(d->rows * parts), parts, threads + 32, 0, s, P);
-    };
-    // Short rows leave most of a wide block waiting for its barriers.
-    if (d->vocab <= kNarrow * V * kBatch)
-        return same ? go(distill_kernel<T, FWD, GRAD, true, kNarrow>, kNarrow)
-                    : go(distill_kernel<T, FWD, GRAD, !GRAD, kNarrow>, kNarrow);
-    return same ? go(distill_kernel<T, FWD, GRAD, true, kWide>, kWide)
-                : go(distill_kernel<T, FWD, GRAD, !GRAD, kWide>, kWide);
+    while (parts < kSizeCluster && bytes > parts * part) parts *= 2;
+    // More while a row's blocks leave SMs idle and its parts keep a vector for each thread.
+    while (parts < kMaxCluster && d->rows * parts < sm_count() && bytes / (2 * parts) >= shape_of(kMedium).threads * 16) parts *= 2;
+    // Short rows leave most of a wide block waiting for its barriers; a single sweep has
+    // nothing to keep in L2.
+    if (bytes <= kNarrowRow) return launch_width<T, FWD, GRAD, kNarrow>(d, P, parts, s);
+    if constexpr (FWD && GRAD)
+        if (bytes / parts > kMediumPart) return launch_width<T, FWD, GRAD, kWide>(d, P, parts, s);
+    return launch_width<T, FWD, GRAD, kMedium>(d, P, parts, s);
 }
 
 Params params_of(const malt_distill_t* d) {
