@@ -76,6 +76,7 @@ embed_forward_kernel(const I* ids, int64_t tokens, int64_t vocab, int64_t dim, c
 // atomic that decides it.  Then it zeroes its rows that no token names.
 constexpr int kSortThreads = 1024;
 constexpr int kSortWarps = kSortThreads / 32;
+constexpr int kSortLoads = 8;               // ids of a lane in flight
 constexpr int kMaxOwned = kSortThreads;     // rows of a block: one thread scans each
 
 // A token in sorted order: its index, its row and the row's range of records.
@@ -106,12 +107,18 @@ embed_sort_kernel(const I* ids, int32_t tokens, int32_t vocab, int32_t owned, To
     const int32_t hi = static_cast<int32_t>(min(static_cast<int64_t>(lo) + per, static_cast<int64_t>(tokens)));
     uint32_t* const mine = place + warp * owned;
     int32_t below = 0;
-#pragma unroll 4
-    for (int64_t i = lo + lane; i < hi; i += 32) {
-        const int64_t id = load_id(ids, i);
-        if (id >= 0 && id < v1) {
-            if (id < v0) ++below;
-            else atomicAdd(mine + (id - v0), 1u);
+    for (int32_t i0 = lo; i0 < hi; i0 += 32 * kSortLoads) {
+        int64_t id[kSortLoads];
+#pragma unroll
+        for (int k = 0; k < kSortLoads; ++k) {
+            const int32_t i = i0 + 32 * k + lane;
+            id[k] = i < hi ? load_id(ids, i) : -1;
+        }
+#pragma unroll
+        for (int k = 0; k < kSortLoads; ++k) {
+            if (id[k] < 0 || id[k] >= v1) continue;
+            if (id[k] < v0) ++below;
+            else atomicAdd(mine + (id[k] - v0), 1u);
         }
     }
     below = __reduce_add_sync(~0u, below);
@@ -149,20 +156,27 @@ embed_sort_kernel(const I* ids, int32_t tokens, int32_t vocab, int32_t owned, To
     if (blockIdx.x == gridDim.x - 1 && threadIdx.x == kSortThreads - 1) *total = s_base + before + incl;
     __syncthreads();
 
-    for (int32_t i0 = lo; i0 < hi; i0 += 32) {
-        const int32_t i = i0 + lane;
-        const int64_t id = i < hi ? load_id(ids, i) : -1;
-        const bool in = id >= v0 && id < v1;
-        const unsigned m = __ballot_sync(~0u, in);
-        if (in) {
-            const int r = static_cast<int>(id - v0);
-            const unsigned peers = __match_any_sync(m, r);
-            const uint32_t first = mine[r];
-            __syncwarp(m);
-            if ((peers & ((1u << lane) - 1)) == 0) mine[r] = first + __popc(peers);
-            __syncwarp(m);
-            const uint32_t at = first + __popc(peers & ((1u << lane) - 1));
-            rec[at] = TokenRecord{i, static_cast<int32_t>(id), row_begin[r], row_end[r]};
+    for (int32_t i0 = lo; i0 < hi; i0 += 32 * kSortLoads) {
+        int64_t id[kSortLoads];
+#pragma unroll
+        for (int k = 0; k < kSortLoads; ++k) {
+            const int32_t i = i0 + 32 * k + lane;
+            id[k] = i < hi ? load_id(ids, i) : -1;
+        }
+#pragma unroll
+        for (int k = 0; k < kSortLoads; ++k) {
+            const bool in = id[k] >= v0 && id[k] < v1;
+            const unsigned m = __ballot_sync(~0u, in);
+            if (in) {
+                const int r = static_cast<int>(id[k] - v0);
+                const unsigned peers = __match_any_sync(m, r), lower = peers & ((1u << lane) - 1);
+                const uint32_t first = mine[r];
+                __syncwarp(m);
+                if (lower == 0) mine[r] = first + __popc(peers);
+                __syncwarp(m);
+                rec[first + __popc(lower)] =
+                    TokenRecord{i0 + 32 * k + lane, static_cast<int32_t>(id[k]), row_begin[r], row_end[r]};
+            }
         }
     }
     if (!fill) return;
@@ -179,6 +193,11 @@ embed_sort_kernel(const I* ids, int32_t tokens, int32_t vocab, int32_t owned, To
 // most `window` tokens is summed by the window that it begins in, whole; a longer
 // one in parts, a part per window, which the join launch adds up.
 constexpr int kSumLoads = 8;        // tokens in flight
+
+template <typename S, int VEC>
+struct alignas(sizeof(S) * VEC) Raw {
+    S v[VEC];
+};
 
 template <typename D, int VEC, int SUB>
 __device__ __forceinline__ void store_row(D* row, int64_t base, int64_t dim, float (&acc)[SUB][VEC], float scale,
@@ -215,92 +234,106 @@ embed_sum_kernel(const TokenRecord* rec, const int32_t* total, int32_t windows, 
     const int32_t a = w * window, b = min(n, a + window);
     if (a >= n) return;
     rec = after_wait(rec);
-    int32_t i = a;
-    {
-        const TokenRecord first = rec[a];
-        if (first.begin < a && first.end - first.begin <= window) i = first.end;    // the window before has it
-    }
-    while (i < b) {
-        const TokenRecord head = rec[i];
-        const bool whole = head.end - head.begin <= window;
-        const int32_t end = whole ? head.end : min(head.end, b);
-        float acc[SUB][VEC] = {};
-        for (int32_t at = i; at < end; at += kSumLoads) {
-            float x[kSumLoads][SUB][VEC];
+    // From the first token that is no tail of a row of the window before, to the end of
+    // the last row that this window sums whole.
+    const TokenRecord head = rec[a], tail = rec[b - 1];
+    const int32_t i0 = head.begin < a && head.end - head.begin <= window ? head.end : a;
+    const int32_t stop = tail.end - tail.begin <= window ? tail.end : b;
+    int64_t column[SUB];            // of the lane's vectors; past the row's end its last one, not stored
+#pragma unroll
+    for (int s = 0; s < SUB; ++s) column[s] = min(base + s * (32 * VEC), dim - VEC);
+    float acc[SUB][VEC] = {};
+    for (int32_t at = i0; at < stop; at += 32) {
+        const TokenRecord mine = rec[min(at + lane, stop - 1)];
+        const int32_t here = min(32, stop - at);
+        // tokens that end a row, or this window's part of it
+        const unsigned ends = __ballot_sync(~0u, lane < here && (at + lane + 1 == mine.end || at + lane + 1 == stop));
+        for (int32_t j0 = 0; j0 < here; j0 += kSumLoads) {
+            Raw<S, VEC> x[kSumLoads][SUB];
 #pragma unroll
             for (int j = 0; j < kSumLoads; ++j) {
-                if (at + j < end) {
-                    const S* const row = dout + static_cast<int64_t>(rec[at + j].token) * dout_ld;
+                const int32_t token = __shfl_sync(~0u, mine.token, min(j0 + j, here - 1));
+                const S* const row = dout + static_cast<int64_t>(token) * dout_ld;
 #pragma unroll
-                    for (int s = 0; s < SUB; ++s) {
-                        const int64_t e = base + s * (32 * VEC);
-                        if (e < dim) load_vec<S, VEC>(row + e, x[j][s]);
-                    }
-                }
+                for (int s = 0; s < SUB; ++s) x[j][s] = *reinterpret_cast<const Raw<S, VEC>*>(row + column[s]);
             }
 #pragma unroll
-            for (int j = 0; j < kSumLoads; ++j)
-                if (at + j < end)
+            for (int j = 0; j < kSumLoads; ++j) {
+                if (j0 + j >= here) break;
+#pragma unroll
+                for (int s = 0; s < SUB; ++s)
+#pragma unroll
+                    for (int k = 0; k < VEC; ++k) acc[s][k] += static_cast<float>(x[j][s].v[k]);
+                if ((ends >> (j0 + j) & 1) == 0) continue;
+                const int32_t row = __shfl_sync(~0u, mine.row, j0 + j), begin = __shfl_sync(~0u, mine.begin, j0 + j);
+                const int32_t end = __shfl_sync(~0u, mine.end, j0 + j);
+                if (end - begin <= window) {
+                    store_row<D, VEC, SUB>(dtable + static_cast<int64_t>(row) * ld, base, dim, acc, scale, accumulate);
+                } else {
+                    // slot 0: the row began in an earlier window; slot 1: it begins in this one
+                    float* const part = parts + (static_cast<int64_t>(w) * 2 + (begin >= a)) * dim;
 #pragma unroll
                     for (int s = 0; s < SUB; ++s)
-#pragma unroll
-                        for (int k = 0; k < VEC; ++k) acc[s][k] += x[j][s][k];
-        }
-        if (whole) {
-            store_row<D, VEC, SUB>(dtable + static_cast<int64_t>(head.row) * ld, base, dim, acc, scale, accumulate);
-        } else {
-            // slot 0: the row began in an earlier window; slot 1: it begins in this one
-            float* const part = parts + (static_cast<int64_t>(w) * 2 + (head.begin >= a)) * dim;
-#pragma unroll
-            for (int s = 0; s < SUB; ++s)
-#pragma unroll
-                for (int k = 0; k < VEC; ++k) {
-                    const int64_t e = base + s * (32 * VEC) + k;
-                    if (e < dim) part[e] = acc[s][k];
+                        if (base + s * (32 * VEC) < dim) store_vec<float, VEC>(part + column[s], acc[s]);
                 }
+#pragma unroll
+                for (int s = 0; s < SUB; ++s)
+#pragma unroll
+                    for (int k = 0; k < VEC; ++k) acc[s][k] = 0.f;
+            }
         }
-        i = end;
     }
 }
 
-// The rows of more than `window` tokens: the parts of each added up by the block of
-// the window it begins in, a warp every kWarps-th part.
+// The rows of more than `window` tokens: a block takes kJoinCols columns of the row that
+// begins last in a window, each warp every kWarps-th of the row's parts.
+constexpr int kJoinCols = 128, kJoinLoads = 4;
 template <typename D>
 __global__ void __launch_bounds__(kThreads)
-embed_join_kernel(const TokenRecord* rec, const int32_t* total, int32_t window, D* dtable, int64_t ld, int64_t dim,
-                  float scale, int accumulate, const float* parts) {
+embed_join_kernel(const TokenRecord* rec, const int32_t* total, int32_t window, int32_t slices, D* dtable, int64_t ld,
+                  int64_t dim, float scale, int accumulate, const float* parts) {
     chain_wait();
     const int32_t n = *after_wait(total);
-    const int32_t w = blockIdx.x;
+    const int32_t w = blockIdx.x / slices;
     const int32_t a = w * window, b = min(n, a + window);
     if (a >= n) return;
     const TokenRecord last = after_wait(rec)[b - 1];
     if (last.end - last.begin <= window || last.begin < a) return;
     parts = after_wait(parts);
     const int32_t w_end = (last.end - 1) / window;
-    __shared__ float sums[kWarps][32];
+    __shared__ float sums[kWarps][kJoinCols];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    D* const row = dtable + static_cast<int64_t>(last.row) * ld;
-    for (int64_t e0 = 0; e0 < dim; e0 += 32) {
-        const int64_t e = e0 + lane;
-        float acc = 0.f;
-        if (e < dim) {
-            for (int32_t k = w + warp; k <= w_end; k += kWarps)
-                acc += parts[(static_cast<int64_t>(k) * 2 + (k == w)) * dim + e];
-        }
-        sums[warp][lane] = acc;
-        __syncthreads();
-        if (warp == 0 && e < dim) {
-            float y[1] = {0.f};
+    const int64_t base = static_cast<int64_t>(blockIdx.x - w * slices) * kJoinCols;
+    constexpr int kCols = kJoinCols / 32;
+    float acc[kCols] = {};
+    for (int32_t k0 = w + warp; k0 <= w_end; k0 += kWarps * kJoinLoads) {
+        float x[kJoinLoads][kCols];
 #pragma unroll
-            for (int k = 0; k < kWarps; ++k) y[0] += sums[k][lane];
-            float old[1] = {0.f};
-            if (accumulate) load_vec<D, 1>(row + e, old);
-            y[0] = fmaf(scale, y[0], old[0]);
-            store_vec<D, 1>(row + e, y);
+        for (int u = 0; u < kJoinLoads; ++u) {
+            const int32_t k = k0 + u * kWarps;
+#pragma unroll
+            for (int c = 0; c < kCols; ++c) {
+                const int64_t e = base + c * 32 + lane;
+                x[u][c] = k <= w_end && e < dim ? parts[(static_cast<int64_t>(k) * 2 + (k == w)) * dim + e] : 0.f;
+            }
         }
-        __syncthreads();
+#pragma unroll
+        for (int u = 0; u < kJoinLoads; ++u)
+#pragma unroll
+            for (int c = 0; c < kCols; ++c) acc[c] += x[u][c];
     }
+#pragma unroll
+    for (int c = 0; c < kCols; ++c) sums[warp][c * 32 + lane] = acc[c];
+    __syncthreads();
+    const int64_t e = base + threadIdx.x;
+    if (threadIdx.x >= kJoinCols || e >= dim) return;
+    float y[1] = {0.f}, old[1] = {0.f};
+#pragma unroll
+    for (int k = 0; k < kWarps; ++k) y[0] += sums[k][threadIdx.x];
+    D* const to = dtable + static_cast<int64_t>(last.row) * ld + e;
+    if (accumulate) load_vec<D, 1>(to, old);
+    y[0] = fmaf(scale, y[0], old[0]);
+    store_vec<D, 1>(to, y);
 }
 
 // ----------------------------------------------------------------------- host
@@ -396,8 +429,11 @@ cudaError_t sums(const malt_embed_t* e, const Workspace& w, uint8_t* ws, int acc
                                     static_cast<const S*>(e->rows), e->rows_ld, dtable, e->table_ld, e->dim,
                                     e->scale, accumulate, parts);
     if (rc != cudaSuccess || e->tokens <= window) return rc;
-    return launch_chained(embed_join_kernel<D>, static_cast<unsigned>(windows), kThreads, 0, s, rec, total, window,
-                          dtable, e->table_ld, e->dim, e->scale, accumulate, static_cast<const float*>(parts));
+    const int64_t cols = (e->dim + kJoinCols - 1) / kJoinCols;
+    if (windows * cols >= (int64_t{1} << 31)) return cudaErrorInvalidValue;
+    return launch_chained(embed_join_kernel<D>, static_cast<unsigned>(windows * cols), kThreads, 0, s, rec, total, window,
+                          static_cast<int32_t>(cols), dtable, e->table_ld, e->dim, e->scale, accumulate,
+                          static_cast<const float*>(parts));
 }
 
 template <typename I>
