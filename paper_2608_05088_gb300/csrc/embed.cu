@@ -5,8 +5,7 @@
 // summed in fp32 in an order that the tokens alone fix: the tokens of a row in
 // their own order, long runs in windows of a fixed length.
 //
-// Both are bound by HBM.  The gradient is written once: rows that no token names
-// are zeroed by the sort launch, the others stored by the launch that sums them.
+// Both are bound by HBM, and every row of the gradient is written once.
 #include <algorithm>
 
 #include <nvtx3/nvToolsExt.h>
@@ -18,6 +17,7 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
+constexpr int kWindow = 16;
 
 // ------------------------------------------------------------------- forward
 // One warp per token and slice of the row; every lane has up to kFwdLoads
@@ -69,13 +69,15 @@ embed_forward_kernel(const I* ids, int64_t tokens, int64_t vocab, int64_t dim, c
 }
 
 // ------------------------------------------------------------ backward: sort
-// Block b owns the table rows [b R, (b + 1) R).  It reads every id, counts those
-// of its rows (per warp, each warp a contiguous run of tokens) and those below its
-// rows, and writes the records of its tokens to their place in the order (row,
+// Block b of n (a power of two) owns the table rows b, b + n, b + 2 n, ...: the ids of
+// frequent tokens, which lie together, are spread over the blocks.  It reads every id, counts those of its
+// rows (per warp, each warp a contiguous run of tokens) and those of the blocks before
+// it, and writes the records of its tokens to their place in the order (block, row,
 // token): no launch has to wait for another block's counts, and the order needs no
 // atomic that decides it.  Then it zeroes its rows that no token names.
 constexpr int kSortThreads = 1024;
 constexpr int kSortWarps = kSortThreads / 32;
+static_assert(kSortWarps == 32, "a warp adds up one value of each warp");
 constexpr int kSortLoads = 8;               // ids of a lane in flight
 constexpr int kMaxOwned = kSortThreads;     // rows of a block: one thread scans each
 
@@ -86,8 +88,8 @@ struct __align__(16) TokenRecord {
 
 template <typename I, typename D, int VEC>
 __global__ void __launch_bounds__(kSortThreads)
-embed_sort_kernel(const I* ids, int32_t tokens, int32_t vocab, int32_t owned, TokenRecord* rec, int32_t* total,
-                  D* dtable, int64_t ld, int64_t dim, int fill) {
+embed_sort_kernel(const I* ids, int32_t tokens, int32_t vocab, int shift, int32_t owned, TokenRecord* rec,
+                  int32_t* total, D* dtable, int64_t ld, int64_t dim, int fill) {
     extern __shared__ uint32_t smem[];
     uint32_t* const place = smem;                               // [kSortWarps][owned]
     int32_t* const row_begin = reinterpret_cast<int32_t*>(smem + kSortWarps * owned);
@@ -96,8 +98,7 @@ embed_sort_kernel(const I* ids, int32_t tokens, int32_t vocab, int32_t owned, To
     __shared__ int32_t s_base;
 
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int32_t v0 = static_cast<int32_t>(blockIdx.x) * owned;
-    const int32_t v1 = min(vocab, v0 + owned);
+    const uint32_t mask = (1u << shift) - 1;
     for (int i = threadIdx.x; i < kSortWarps * owned; i += kSortThreads) place[i] = 0;
     __syncthreads();
     chain_wait();
@@ -116,9 +117,10 @@ embed_sort_kernel(const I* ids, int32_t tokens, int32_t vocab, int32_t owned, To
         }
 #pragma unroll
         for (int k = 0; k < kSortLoads; ++k) {
-            if (id[k] < 0 || id[k] >= v1) continue;
-            if (id[k] < v0) ++below;
-            else atomicAdd(mine + (id[k] - v0), 1u);
+            if (static_cast<uint64_t>(id[k]) >= static_cast<uint64_t>(vocab)) continue;     // negative ones too
+            const uint32_t of = static_cast<uint32_t>(id[k]) & mask;
+            below += of < blockIdx.x;
+            if (of == blockIdx.x) atomicAdd(mine + (static_cast<uint32_t>(id[k]) >> shift), 1u);
         }
     }
     below = __reduce_add_sync(~0u, below);
@@ -132,6 +134,7 @@ embed_sort_kernel(const I* ids, int32_t tokens, int32_t vocab, int32_t owned, To
     // Exclusive sums: over the rows, and within a row over the warps.
     int32_t count = 0;
     if (threadIdx.x < owned)
+#pragma unroll
         for (int w = 0; w < kSortWarps; ++w) count += place[w * owned + threadIdx.x];
     int32_t incl = count;
 #pragma unroll
@@ -147,6 +150,7 @@ embed_sort_kernel(const I* ids, int32_t tokens, int32_t vocab, int32_t owned, To
         int32_t at = s_base + before + incl - count;
         row_begin[threadIdx.x] = at;
         row_end[threadIdx.x] = at + count;
+#pragma unroll 8
         for (int w = 0; w < kSortWarps; ++w) {
             const int32_t n = place[w * owned + threadIdx.x];
             place[w * owned + threadIdx.x] = at;
@@ -165,10 +169,11 @@ embed_sort_kernel(const I* ids, int32_t tokens, int32_t vocab, int32_t owned, To
         }
 #pragma unroll
         for (int k = 0; k < kSortLoads; ++k) {
-            const bool in = id[k] >= v0 && id[k] < v1;
+            const bool in = static_cast<uint64_t>(id[k]) < static_cast<uint64_t>(vocab) &&
+                            (static_cast<uint32_t>(id[k]) & mask) == blockIdx.x;
             const unsigned m = __ballot_sync(~0u, in);
             if (in) {
-                const int r = static_cast<int>(id[k] - v0);
+                const uint32_t r = static_cast<uint32_t>(id[k]) >> shift;
                 const unsigned peers = __match_any_sync(m, r), lower = peers & ((1u << lane) - 1);
                 const uint32_t first = mine[r];
                 __syncwarp(m);
@@ -181,9 +186,9 @@ embed_sort_kernel(const I* ids, int32_t tokens, int32_t vocab, int32_t owned, To
     }
     if (!fill) return;
     const float zero[VEC] = {};
-    for (int r = warp; r < v1 - v0; r += kSortWarps) {
+    for (int64_t r = warp; (r << shift) + blockIdx.x < vocab; r += kSortWarps) {
         if (row_begin[r] != row_end[r]) continue;
-        D* const row = dtable + static_cast<int64_t>(v0 + r) * ld;
+        D* const row = dtable + ((r << shift) + blockIdx.x) * ld;
         for (int64_t e = lane * VEC; e < dim; e += 32 * VEC) store_vec<D, VEC>(row + e, zero);
     }
 }
@@ -192,45 +197,25 @@ embed_sort_kernel(const I* ids, int32_t tokens, int32_t vocab, int32_t owned, To
 // A warp takes a window of the sorted tokens and a slice of the row.  A row of at
 // most `window` tokens is summed by the window that it begins in, whole; a longer
 // one in parts, a part per window, which the join launch adds up.
-constexpr int kSumLoads = 8;        // tokens in flight
 
 template <typename S, int VEC>
 struct alignas(sizeof(S) * VEC) Raw {
     S v[VEC];
 };
 
-template <typename D, int VEC, int SUB>
-__device__ __forceinline__ void store_row(D* row, int64_t base, int64_t dim, float (&acc)[SUB][VEC], float scale,
-                                          int accumulate) {
-#pragma unroll
-    for (int s = 0; s < SUB; ++s) {
-        const int64_t e = base + s * (32 * VEC);
-        if (e >= dim) continue;
-        float y[VEC];
-        if (accumulate) {
-            load_vec<D, VEC>(row + e, y);
-#pragma unroll
-            for (int i = 0; i < VEC; ++i) y[i] = fmaf(scale, acc[s][i], y[i]);
-        } else {
-#pragma unroll
-            for (int i = 0; i < VEC; ++i) y[i] = scale * acc[s][i];
-        }
-        store_vec<D, VEC>(row + e, y);
-    }
-}
-
-template <typename S, typename D, int VEC, int SUB>
+// ADD: to what the table holds, whose rows are loaded with the tokens that end them.
+template <typename S, typename D, bool ADD, int VEC, int SUB>
 __global__ void __launch_bounds__(kThreads)
 embed_sum_kernel(const TokenRecord* rec, const int32_t* total, int32_t windows, int32_t window, int32_t slices,
-                 const S* dout, int64_t dout_ld, D* dtable, int64_t ld, int64_t dim, float scale, int accumulate,
-                 float* parts) {
+                 const S* dout, int64_t dout_ld, D* dtable, int64_t ld, int64_t dim, float scale, float* parts) {
+    constexpr int kSumLoads = ADD ? 8 : 16;      // tokens in flight
     chain_wait();
+    const int32_t n = *after_wait(total);
     const int lane = threadIdx.x & 31;
     const int64_t item = static_cast<int64_t>(blockIdx.x) * kWarps + (threadIdx.x >> 5);
     const int32_t w = static_cast<int32_t>(item / slices);
     if (w >= windows) return;
     const int64_t base = (item - static_cast<int64_t>(w) * slices) * (32 * VEC * SUB) + lane * VEC;
-    const int32_t n = *after_wait(total);
     const int32_t a = w * window, b = min(n, a + window);
     if (a >= n) return;
     rec = after_wait(rec);
@@ -250,12 +235,18 @@ embed_sum_kernel(const TokenRecord* rec, const int32_t* total, int32_t windows, 
         const unsigned ends = __ballot_sync(~0u, lane < here && (at + lane + 1 == mine.end || at + lane + 1 == stop));
         for (int32_t j0 = 0; j0 < here; j0 += kSumLoads) {
             Raw<S, VEC> x[kSumLoads][SUB];
+            Raw<D, VEC> old[ADD ? kSumLoads : 1][SUB];
 #pragma unroll
             for (int j = 0; j < kSumLoads; ++j) {
                 const int32_t token = __shfl_sync(~0u, mine.token, min(j0 + j, here - 1));
                 const S* const row = dout + static_cast<int64_t>(token) * dout_ld;
 #pragma unroll
                 for (int s = 0; s < SUB; ++s) x[j][s] = *reinterpret_cast<const Raw<S, VEC>*>(row + column[s]);
+                if (ADD && j0 + j < here && (ends >> (j0 + j) & 1)) {
+                    const D* const to = dtable + static_cast<int64_t>(__shfl_sync(~0u, mine.row, j0 + j)) * ld;
+#pragma unroll
+                    for (int s = 0; s < SUB; ++s) old[j % (ADD ? kSumLoads : 1)][s] = *reinterpret_cast<const Raw<D, VEC>*>(to + column[s]);
+                }
             }
 #pragma unroll
             for (int j = 0; j < kSumLoads; ++j) {
@@ -268,7 +259,16 @@ embed_sum_kernel(const TokenRecord* rec, const int32_t* total, int32_t windows, 
                 const int32_t row = __shfl_sync(~0u, mine.row, j0 + j), begin = __shfl_sync(~0u, mine.begin, j0 + j);
                 const int32_t end = __shfl_sync(~0u, mine.end, j0 + j);
                 if (end - begin <= window) {
-                    store_row<D, VEC, SUB>(dtable + static_cast<int64_t>(row) * ld, base, dim, acc, scale, accumulate);
+                    D* const to = dtable + static_cast<int64_t>(row) * ld;
+#pragma unroll
+                    for (int s = 0; s < SUB; ++s) {
+                        float y[VEC];
+#pragma unroll
+                        for (int k = 0; k < VEC; ++k)
+                            y[k] = ADD ? fmaf(scale, acc[s][k], static_cast<float>(old[j % (ADD ? kSumLoads : 1)][s].v[k]))
+                                       : scale * acc[s][k];
+                        if (base + s * (32 * VEC) < dim) store_vec<D, VEC>(to + column[s], y);
+                    }
                 } else {
                     // slot 0: the row began in an earlier window; slot 1: it begins in this one
                     float* const part = parts + (static_cast<int64_t>(w) * 2 + (begin >= a)) * dim;
@@ -285,62 +285,74 @@ embed_sum_kernel(const TokenRecord* rec, const int32_t* total, int32_t windows, 
     }
 }
 
-// The rows of more than `window` tokens: a block takes kJoinCols columns of the row that
-// begins last in a window, each warp every kWarps-th of the row's parts.
+// The rows of more than `window` tokens: a block looks at kWarps windows, and takes
+// kJoinCols columns of each such row that begins last in one of them, each warp every
+// kWarps-th of the row's parts.
 constexpr int kJoinCols = 128, kJoinLoads = 4;
 template <typename D>
 __global__ void __launch_bounds__(kThreads)
-embed_join_kernel(const TokenRecord* rec, const int32_t* total, int32_t window, int32_t slices, D* dtable, int64_t ld,
-                  int64_t dim, float scale, int accumulate, const float* parts) {
+embed_join_kernel(const TokenRecord* rec, const int32_t* total, int32_t windows, int32_t window, int32_t slices,
+                  D* dtable, int64_t ld, int64_t dim, float scale, int accumulate, const float* parts) {
+    __shared__ TokenRecord last[kWarps];
+    __shared__ float sums[kWarps][kJoinCols];
+    constexpr int kCols = kJoinCols / 32;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int32_t group = blockIdx.x / slices;
+    const int64_t base = static_cast<int64_t>(blockIdx.x - group * slices) * kJoinCols;
     chain_wait();
     const int32_t n = *after_wait(total);
-    const int32_t w = blockIdx.x / slices;
-    const int32_t a = w * window, b = min(n, a + window);
-    if (a >= n) return;
-    const TokenRecord last = after_wait(rec)[b - 1];
-    if (last.end - last.begin <= window || last.begin < a) return;
-    parts = after_wait(parts);
-    const int32_t w_end = (last.end - 1) / window;
-    __shared__ float sums[kWarps][kJoinCols];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int64_t base = static_cast<int64_t>(blockIdx.x - w * slices) * kJoinCols;
-    constexpr int kCols = kJoinCols / 32;
-    float acc[kCols] = {};
-    for (int32_t k0 = w + warp; k0 <= w_end; k0 += kWarps * kJoinLoads) {
-        float x[kJoinLoads][kCols];
-#pragma unroll
-        for (int u = 0; u < kJoinLoads; ++u) {
-            const int32_t k = k0 + u * kWarps;
-#pragma unroll
-            for (int c = 0; c < kCols; ++c) {
-                const int64_t e = base + c * 32 + lane;
-                x[u][c] = k <= w_end && e < dim ? parts[(static_cast<int64_t>(k) * 2 + (k == w)) * dim + e] : 0.f;
-            }
-        }
-#pragma unroll
-        for (int u = 0; u < kJoinLoads; ++u)
-#pragma unroll
-            for (int c = 0; c < kCols; ++c) acc[c] += x[u][c];
+    if (threadIdx.x < kWarps) {
+        const int64_t a = (static_cast<int64_t>(group) * kWarps + threadIdx.x) * window;
+        TokenRecord r = {0, 0, 0, 0};
+        if (a < n) r = after_wait(rec)[min(static_cast<int64_t>(n), a + window) - 1];
+        if (r.begin < a) r.end = r.begin;       // another window's
+        last[threadIdx.x] = r;
     }
-#pragma unroll
-    for (int c = 0; c < kCols; ++c) sums[warp][c * 32 + lane] = acc[c];
     __syncthreads();
-    const int64_t e = base + threadIdx.x;
-    if (threadIdx.x >= kJoinCols || e >= dim) return;
-    float y[1] = {0.f}, old[1] = {0.f};
+    parts = after_wait(parts);
+    for (int i = 0; i < kWarps; ++i) {
+        const TokenRecord r = last[i];
+        if (r.end - r.begin <= window) continue;
+        const int32_t w = group * kWarps + i, w_end = (r.end - 1) / window;
+        float acc[kCols] = {};
+        for (int32_t k0 = w + warp; k0 <= w_end; k0 += kWarps * kJoinLoads) {
+            float x[kJoinLoads][kCols];
 #pragma unroll
-    for (int k = 0; k < kWarps; ++k) y[0] += sums[k][threadIdx.x];
-    D* const to = dtable + static_cast<int64_t>(last.row) * ld + e;
-    if (accumulate) load_vec<D, 1>(to, old);
-    y[0] = fmaf(scale, y[0], old[0]);
-    store_vec<D, 1>(to, y);
+            for (int u = 0; u < kJoinLoads; ++u) {
+                const int32_t k = k0 + u * kWarps;
+#pragma unroll
+                for (int c = 0; c < kCols; ++c) {
+                    const int64_t e = base + c * 32 + lane;
+                    x[u][c] = k <= w_end && e < dim ? parts[(static_cast<int64_t>(k) * 2 + (k == w)) * dim + e] : 0.f;
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < kJoinLoads; ++u)
+#pragma unroll
+                for (int c = 0; c < kCols; ++c) acc[c] += x[u][c];
+        }
+        __syncthreads();
+#pragma unroll
+        for (int c = 0; c < kCols; ++c) sums[warp][c * 32 + lane] = acc[c];
+        __syncthreads();
+        const int64_t e = base + threadIdx.x;
+        if (threadIdx.x < kJoinCols && e < dim) {
+            float y[1] = {0.f}, old[1] = {0.f};
+#pragma unroll
+            for (int k = 0; k < kWarps; ++k) y[0] += sums[k][threadIdx.x];
+            D* const to = dtable + static_cast<int64_t>(r.row) * ld + e;
+            if (accumulate) load_vec<D, 1>(to, old);
+            y[0] = fmaf(scale, y[0], old[0]);
+            store_vec<D, 1>(to, y);
+        }
+    }
 }
 
 // ----------------------------------------------------------------------- host
-// Windows of the sorted tokens: 32 tokens, more where that would make over 1024
+// Windows of the sorted tokens: kWindow tokens, more where that would make over 1024
 // windows (a row's parts are then at most 1024).
 int32_t window_length(int64_t tokens) {
-    int64_t w = 32;
+    int64_t w = kWindow;
     while (tokens > w * 1024) w *= 2;
     return static_cast<int32_t>(w);
 }
@@ -396,10 +408,14 @@ cudaError_t forward(const malt_embed_t* e, cudaStream_t s) {
 }
 
 template <typename I, typename D, int VEC>
-cudaError_t sort(const malt_embed_t* e, const Workspace& w, uint8_t* ws, int fill, cudaStream_t s) {
-    const int64_t blocks0 = std::max<int64_t>(sm_count(), (e->vocab + kMaxOwned - 1) / kMaxOwned);
-    const int32_t owned = static_cast<int32_t>((e->vocab + blocks0 - 1) / blocks0);
-    const unsigned blocks = static_cast<unsigned>((e->vocab + owned - 1) / owned);
+cudaError_t sort(const malt_embed_t* e, const Workspace& w, uint8_t* ws, bool add, cudaStream_t s) {
+    // Of the powers of two the largest that the SMs hold at once, more for a table of more
+    // rows than these can own.
+    int shift = 0;
+    while ((2 << shift) <= sm_count()) ++shift;
+    while ((int64_t{kMaxOwned} << shift) < e->vocab) ++shift;
+    const int64_t blocks = int64_t{1} << shift;
+    const int32_t owned = static_cast<int32_t>((e->vocab + blocks - 1) / blocks);
     const size_t smem = (kSortWarps + 2) * sizeof(uint32_t) * static_cast<size_t>(owned);
     auto* const kernel = embed_sort_kernel<I, D, VEC>;
     if (smem > 48 * 1024) {
@@ -407,32 +423,36 @@ cudaError_t sort(const malt_embed_t* e, const Workspace& w, uint8_t* ws, int fil
                                                     static_cast<int>(smem));
         if (rc != cudaSuccess) { cudaGetLastError(); return rc; }
     }
-    return launch_chained(kernel, blocks, kSortThreads, smem, s, static_cast<const I*>(e->ids),
-                          static_cast<int32_t>(e->tokens), static_cast<int32_t>(e->vocab), owned,
+    return launch_chained(kernel, static_cast<unsigned>(blocks), kSortThreads, smem, s, static_cast<const I*>(e->ids),
+                          static_cast<int32_t>(e->tokens), static_cast<int32_t>(e->vocab), shift, owned,
                           reinterpret_cast<TokenRecord*>(ws + w.rec), reinterpret_cast<int32_t*>(ws + w.total),
-                          static_cast<D*>(e->table), e->table_ld, e->dim, fill);
+                          static_cast<D*>(e->table), e->table_ld, e->dim, add ? 0 : 1);
 }
 
-template <typename S, typename D, int VEC, int SUB>
-cudaError_t sums(const malt_embed_t* e, const Workspace& w, uint8_t* ws, int accumulate, cudaStream_t s) {
+template <typename I, typename D>
+cudaError_t sort_types(const malt_embed_t* e, const Workspace& w, uint8_t* ws, bool add, cudaStream_t s) {
+    constexpr int V = 16 / sizeof(D);
+    return e->table_ld % V == 0 && e->dim % V == 0 && aligned_to(e->table, 16) ? sort<I, D, V>(e, w, ws, add, s)
+                                                                                : sort<I, D, 1>(e, w, ws, add, s);
+}
+
+template <typename S, typename D, bool ADD, int VEC, int SUB>
+cudaError_t sums(const malt_embed_t* e, const Workspace& w, uint8_t* ws, cudaStream_t s) {
     const int32_t window = window_length(e->tokens);
     const int32_t windows = static_cast<int32_t>((e->tokens + window - 1) / window);
     const int64_t slices = (e->dim + 32 * VEC * SUB - 1) / (32 * VEC * SUB);
-    const int64_t blocks = (windows * slices + kWarps - 1) / kWarps;
-    if (blocks >= (int64_t{1} << 31)) return cudaErrorInvalidValue;
+    const int64_t sum_blocks = (windows * slices + kWarps - 1) / kWarps;
+    const int64_t cols = (e->dim + kJoinCols - 1) / kJoinCols, groups = (windows + kWarps - 1) / kWarps;
+    if (sum_blocks >= (int64_t{1} << 31) || groups * cols >= (int64_t{1} << 31)) return cudaErrorInvalidValue;
     const TokenRecord* const rec = reinterpret_cast<TokenRecord*>(ws + w.rec);
     const int32_t* const total = reinterpret_cast<int32_t*>(ws + w.total);
     float* const parts = reinterpret_cast<float*>(ws + w.parts);
     D* const dtable = static_cast<D*>(e->table);
-    cudaError_t rc = launch_chained(embed_sum_kernel<S, D, VEC, SUB>, static_cast<unsigned>(blocks), kThreads, 0, s,
-                                    rec, total, windows, window, static_cast<int32_t>(slices),
-                                    static_cast<const S*>(e->rows), e->rows_ld, dtable, e->table_ld, e->dim,
-                                    e->scale, accumulate, parts);
+    cudaError_t rc = launch_chained(embed_sum_kernel<S, D, ADD, VEC, SUB>, static_cast<unsigned>(sum_blocks), kThreads, 0, s, rec,
+                                    total, windows, window, static_cast<int32_t>(slices), static_cast<const S*>(e->rows), e->rows_ld, dtable, e->table_ld, e->dim, e->scale, parts);
     if (rc != cudaSuccess || e->tokens <= window) return rc;
-    const int64_t cols = (e->dim + kJoinCols - 1) / kJoinCols;
-    if (windows * cols >= (int64_t{1} << 31)) return cudaErrorInvalidValue;
-    return launch_chained(embed_join_kernel<D>, static_cast<unsigned>(windows * cols), kThreads, 0, s, rec, total, window,
-                          static_cast<int32_t>(cols), dtable, e->table_ld, e->dim, e->scale, accumulate,
+    return launch_chained(embed_join_kernel<D>, static_cast<unsigned>(groups * cols), kThreads, 0, s, rec, total,
+                          windows, window, static_cast<int32_t>(cols), dtable, e->table_ld, e->dim, e->scale, ADD ? 1 : 0,
                           static_cast<const float*>(parts));
 }
 
@@ -445,16 +465,10 @@ cudaError_t forward_types(const malt_embed_t* e, cudaStream_t s) {
     return vectors(e, 4) ? forward<I, float, float, 4>(e, s) : forward<I, float, float, 1>(e, s);
 }
 
-template <typename I, typename D>
-cudaError_t sort_types(const malt_embed_t* e, const Workspace& w, uint8_t* ws, int fill, cudaStream_t s) {
-    constexpr int V = 16 / sizeof(D);
-    return e->table_ld % V == 0 && e->dim % V == 0 && aligned_to(e->table, 16) ? sort<I, D, V>(e, w, ws, fill, s)
-                                                                                : sort<I, D, 1>(e, w, ws, fill, s);
-}
-
 template <typename S, typename D>
-cudaError_t sums_types(const malt_embed_t* e, const Workspace& w, uint8_t* ws, int accumulate, cudaStream_t s) {
-    return vectors(e, 4) ? sums<S, D, 4, 2>(e, w, ws, accumulate, s) : sums<S, D, 1, 4>(e, w, ws, accumulate, s);
+cudaError_t sums_types(const malt_embed_t* e, const Workspace& w, uint8_t* ws, bool add, cudaStream_t s) {
+    if (vectors(e, 4)) return add ? sums<S, D, true, 4, 1>(e, w, ws, s) : sums<S, D, false, 4, 1>(e, w, ws, s);
+    return add ? sums<S, D, true, 1, 2>(e, w, ws, s) : sums<S, D, false, 1, 2>(e, w, ws, s);
 }
 
 }  // namespace
@@ -489,13 +503,13 @@ int malt_embed_backward(const malt_embed_t* e, int32_t accumulate, void* workspa
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     uint8_t* const ws = static_cast<uint8_t*>(workspace);
     nvtxRangePushA("malt_embed_backward");
-    const int fill = accumulate ? 0 : 1;
-    const bool i32 = e->ids_dtype == MALT_I32, tb = e->table_dtype == MALT_BF16, rb = e->rows_dtype == MALT_BF16;
-    cudaError_t c = i32 ? (tb ? sort_types<int32_t, bf16>(e, w, ws, fill, s) : sort_types<int32_t, float>(e, w, ws, fill, s))
-                        : (tb ? sort_types<int64_t, bf16>(e, w, ws, fill, s) : sort_types<int64_t, float>(e, w, ws, fill, s));
+    const bool tb = e->table_dtype == MALT_BF16, rb = e->rows_dtype == MALT_BF16, add = accumulate != 0;
+    const bool i32 = e->ids_dtype == MALT_I32;
+    cudaError_t c = i32 ? (tb ? sort_types<int32_t, bf16>(e, w, ws, add, s) : sort_types<int32_t, float>(e, w, ws, add, s))
+                        : (tb ? sort_types<int64_t, bf16>(e, w, ws, add, s) : sort_types<int64_t, float>(e, w, ws, add, s));
     if (c == cudaSuccess && e->tokens > 0)
-        c = rb ? (tb ? sums_types<bf16, bf16>(e, w, ws, accumulate != 0, s) : sums_types<bf16, float>(e, w, ws, accumulate != 0, s))
-               : (tb ? sums_types<float, bf16>(e, w, ws, accumulate != 0, s) : sums_types<float, float>(e, w, ws, accumulate != 0, s));
+        c = rb ? (tb ? sums_types<bf16, bf16>(e, w, ws, add, s) : sums_types<bf16, float>(e, w, ws, add, s))
+               : (tb ? sums_types<float, bf16>(e, w, ws, add, s) : sums_types<float, float>(e, w, ws, add, s));
     nvtxRangePop();
     return cuda_status(c, "malt_embed_backward");
 }

@@ -9,6 +9,10 @@ without synchronising.  Tensors live on the current CUDA device; only the last
 dimension has to be contiguous where nothing else is said.  With a `stream` other
 than the current one, the caller orders its inputs and the use of its outputs; memory
 allocated here is marked as used on that stream.
+
+For a few tokens the time of a call is the host's, so the checks read each property
+of a tensor once, the current device and stream come from torch._C, without the Python
+objects around them, and outputs come from the cheapest of torch's allocating calls.
 """
 from __future__ import annotations
 
@@ -27,27 +31,34 @@ _HEADS = struct.Struct("Pqqqq")
 _DISTILL = struct.Struct("PqqqiiPqPqqPif")
 
 
+# The raw handle of a device's current stream, and the current device.
+_current_stream = torch._C._cuda_getCurrentRawStream
+_current_device = torch._C._cuda_getDevice
+
+
 def _check(code: int, where: str):
     if code != malt.MALT_OK:
         raise malt.MaltError(code, where)
 
 
-def _on_device(**tensors):
-    """The tensors (None entries aside) are CUDA tensors of the current device."""
-    for name, t in tensors.items():
-        if t is not None and not t.is_cuda:
-            raise ValueError(f"{name} must be a CUDA tensor, not on {t.device}")
-    dev = torch.cuda.current_device()
-    for name, t in tensors.items():
+def _device(names, *tensors):
+    """The current CUDA device, which all tensors (None entries aside) are on."""
+    dev = tensors[0].get_device()
+    for t in tensors:
         if t is not None and t.get_device() != dev:
-            raise ValueError(f"{name} must be on the current CUDA device (cuda:{dev}), not {t.device}")
+            dev = -1
+            break
+    if dev < 0 or dev != _current_device():
+        where = {n: str(t.device) for n, t in zip(names.split(), tensors) if t is not None}
+        raise ValueError(f"tensors must be on the current CUDA device: {where}")
+    return dev
 
 
-def _stream(stream, *allocated):
+def _stream(dev, stream, *allocated):
     """The raw stream; memory allocated for this call is kept for it."""
-    current = torch.cuda.current_stream()
-    if stream is None or stream == current:
-        return current.cuda_stream
+    current = _current_stream(dev)
+    if stream is None or stream.cuda_stream == current:
+        return current
     for t in allocated:
         if t is not None:
             t.record_stream(stream)
@@ -96,7 +107,7 @@ def embed(table, ids, scale: float = 1.0, dtype=None, out=None, stream=None):
     """scale * table[ids], of shape ids.shape + (dim,) in `dtype` (default: the
     table's).  A negative id is padding (a zero row); an id past the table gives
     a NaN row.  ids must be contiguous."""
-    _on_device(table=table, ids=ids, out=out)
+    dev = _device("table ids out", table, ids, out)
     if table.dim() != 2:
         raise ValueError("table must be a vocab x dim matrix")
     if not ids.is_contiguous():
@@ -110,7 +121,7 @@ def embed(table, ids, scale: float = 1.0, dtype=None, out=None, stream=None):
     e = _EMBED.pack(ids.data_ptr(), _index_code("ids", ids), _float_code("table", table), _float_code("out", out),
                     scale, ids.numel(), vocab, dim, table.data_ptr(), _row_stride("table", table, dim),
                     out.data_ptr(), _row_stride("out", out, dim))
-    _check(malt.load().malt_embed_forward(e, _stream(stream, out)), "malt_embed_forward")
+    _check(malt.load().malt_embed_forward(e, _stream(dev, stream, out)), "malt_embed_forward")
     return out
 
 
@@ -120,7 +131,7 @@ def embed_grad(dout, ids, vocab: int, scale: float = 1.0, dtype=None, out=None, 
     id is v.  Returns a vocab x dim matrix in `dtype` (default: float32), every row
     written; with `accumulate` the sums are added to `out` instead (only rows that
     occur are touched)."""
-    _on_device(dout=dout, ids=ids, out=out)
+    dev = _device("dout ids out", dout, ids, out)
     if not ids.is_contiguous():
         raise ValueError("ids must be contiguous")
     if dout.dim() < 1 or dout.shape[:-1] != ids.shape:
@@ -139,52 +150,67 @@ def embed_grad(dout, ids, vocab: int, scale: float = 1.0, dtype=None, out=None, 
     e = _EMBED.pack(ids.data_ptr(), _index_code("ids", ids), _float_code("out", out), _float_code("dout", dout),
                     scale, n, vocab, dim, out.data_ptr(), _row_stride("out", out, dim),
                     dout.data_ptr(), _row_stride("dout", dout, dim))
-    _check(lib.malt_embed_backward(e, 1 if accumulate else 0, ws.data_ptr(), size, _stream(stream, out, ws)),
+    _check(lib.malt_embed_backward(e, 1 if accumulate else 0, ws.data_ptr(), size, _stream(dev, stream, out, ws)),
            "malt_embed_backward")
     return out
 
 
 # ------------------------------------------------- norms of queries and keys
 
-def _heads(name, t, like=None):
-    """malt_heads_t of a [batch, seq, heads, dim] or [tokens, heads, dim] tensor."""
-    if like is not None and (t.shape != like.shape or t.dtype != like.dtype):
+def _like(name, t, like):
+    """t, given for something of like's shape and dtype, or memory for it."""
+    if t is None:
+        return torch.empty_like(like)
+    if t.shape != like.shape or t.dtype != like.dtype:
         raise ValueError(f"{name} has shape {tuple(t.shape)} and dtype {t.dtype}, expected {tuple(like.shape)} "
                          f"and {like.dtype}")
-    st = t.stride()
-    if st[-1] != 1 and t.shape[-1] > 1:
-        raise ValueError(f"the heads of {name} must be contiguous")
-    return _HEADS.pack(t.data_ptr(), t.shape[-2], st[0] if len(st) == 4 else 0, st[-3], st[-2])
+    if 0 in t.stride() and not t.is_contiguous():
+        raise ValueError(f"{name} has overlapping entries")
+    return t
+
+
+def _heads(t):
+    """malt_heads_t of a [batch, seq, heads, dim] or [tokens, heads, dim] tensor."""
+    st, shape = t.stride(), t.shape
+    if st[-1] != 1 and shape[-1] > 1:
+        raise ValueError("the entries of a head must be contiguous")
+    if len(st) == 4:
+        return _HEADS.pack(t.data_ptr(), shape[2], st[0], st[1], st[2])
+    return _HEADS.pack(t.data_ptr(), shape[1], 0, st[0], st[1])
 
 
 def _qk_params(q, k, q_gain, k_gain, cos, sin, positions, eps, interleaved):
-    if q.dim() not in (3, 4) or k.dim() != q.dim():
+    shape, k_shape = q.shape, k.shape
+    rank, dim = len(shape), shape[-1]
+    if rank not in (3, 4) or len(k_shape) != rank:
         raise ValueError("q and k must be [batch, seq, heads, dim] or [tokens, heads, dim] tensors")
-    dim = q.shape[-1]
-    if k.shape[:-2] != q.shape[:-2] or k.shape[-1] != dim or k.dtype != q.dtype:
-        raise ValueError(f"q {tuple(q.shape)} {q.dtype} and k {tuple(k.shape)} {k.dtype} differ in more than heads")
-    batch, seq = (1, q.shape[0]) if q.dim() == 3 else q.shape[:2]
-    if (cos.dim() != 2 or cos.shape != sin.shape or cos.dtype != torch.float32 or sin.dtype != torch.float32
+    if k_shape[:-2] != shape[:-2] or k_shape[-1] != dim or k.dtype != q.dtype:
+        raise ValueError(f"q {tuple(shape)} {q.dtype} and k {tuple(k_shape)} {k.dtype} differ in more than heads")
+    batch, seq = (1, shape[0]) if rank == 3 else shape[:2]
+    rows, pairs = cos.shape if cos.dim() == 2 else (0, -1)
+    if (pairs < 0 or cos.shape != sin.shape or cos.dtype != torch.float32 or sin.dtype != torch.float32
             or not cos.is_contiguous() or not sin.is_contiguous()):
         raise ValueError("cos and sin must be contiguous float32 matrices of one shape")
     gain_type = malt.MALT_F32
     for name, g in (("q_gain", q_gain), ("k_gain", k_gain)):
-        _vector(name, g, dim, tuple(_FLOATS))
         if g is not None:
-            gain_type = _FLOATS[g.dtype]
+            gain_type = _float_code(name, g)
+            if g.numel() != dim or not g.is_contiguous():
+                raise ValueError(f"{name} must be a contiguous vector of {dim} entries")
     if q_gain is not None and k_gain is not None and q_gain.dtype != k_gain.dtype:
         raise ValueError("q_gain and k_gain must have one dtype")
     stride = index = 0
     if positions is not None:
         index = _index_code("positions", positions)
-        if positions.shape == (batch, seq) and positions.dim() == 2:
-            stride = positions.stride(0)
-        elif positions.shape != (seq,):
-            raise ValueError(f"positions has shape {tuple(positions.shape)}, expected {(batch, seq)} or {(seq,)}")
-        if seq > 1 and positions.stride(-1) != 1:
+        p_shape, p_stride = positions.shape, positions.stride()
+        if p_shape == (batch, seq):
+            stride = p_stride[0]
+        elif p_shape != (seq,):
+            raise ValueError(f"positions has shape {tuple(p_shape)}, expected {(batch, seq)} or {(seq,)}")
+        if seq > 1 and p_stride[-1] != 1:
             raise ValueError("the last dimension of positions must be contiguous")
-    return _QK.pack(_float_code("q", q), gain_type, dim, 2 * cos.shape[1], 1 if interleaved else 0, eps, batch, seq,
-                    _pointer(positions), index, 0, stride, cos.data_ptr(), sin.data_ptr(), cos.shape[0],
+    return _QK.pack(_float_code("q", q), gain_type, dim, 2 * pairs, 1 if interleaved else 0, eps, batch, seq,
+                    _pointer(positions), index, 0, stride, cos.data_ptr(), sin.data_ptr(), rows,
                     _pointer(q_gain), _pointer(k_gain))
 
 
@@ -197,13 +223,12 @@ def qk_norm(q, k, q_gain, k_gain, cos, sin, positions=None, eps: float = 1e-6, i
     dimension; cos, sin: [positions, pairs]; positions: [batch, seq] or [seq] ([tokens]),
     default 0 .. seq-1.  Pairs are (i, pairs + i), or (2i, 2i+1) when interleaved.
     Returns (q_out, k_out); each may be given, also as its input itself."""
-    _on_device(q=q, k=k, q_gain=q_gain, k_gain=k_gain, cos=cos, sin=sin, positions=positions, q_out=q_out, k_out=k_out)
+    dev = _device("q k q_gain k_gain cos sin positions q_out k_out", q, k, q_gain, k_gain, cos, sin, positions, q_out,
+                  k_out)
     p = _qk_params(q, k, q_gain, k_gain, cos, sin, positions, eps, interleaved)
-    q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device) if q_out is None else q_out
-    k_out = torch.empty(k.shape, dtype=k.dtype, device=k.device) if k_out is None else k_out
-    _check(malt.load().malt_qk_norm_forward(p, _heads("q", q), _heads("k", k), _heads("q_out", q_out, q),
-                                            _heads("k_out", k_out, k), _stream(stream, q_out, k_out)),
-           "malt_qk_norm_forward")
+    q_out, k_out = _like("q_out", q_out, q), _like("k_out", k_out, k)
+    _check(malt.load().malt_qk_norm_forward(p, _heads(q), _heads(k), _heads(q_out), _heads(k_out),
+                                            _stream(dev, stream, q_out, k_out)), "malt_qk_norm_forward")
     return q_out, k_out
 
 
@@ -212,21 +237,21 @@ def qk_norm_grad(dq_out, dk_out, q, k, q_gain, k_gain, cos, sin, positions=None,
     """The gradient of qk_norm from those of its outputs and its own arguments.  Returns
     (dq, dk, dq_gain, dk_gain), the gains' gradients in float32 (None for a gain that is None); dq
     and dk may be given, also as dq_out and dk_out themselves."""
-    _on_device(dq_out=dq_out, dk_out=dk_out, q=q, k=k, q_gain=q_gain, k_gain=k_gain, cos=cos, sin=sin,
-               positions=positions, dq=dq, dk=dk)
+    dev = _device("q k dq_out dk_out q_gain k_gain cos sin positions dq dk", q, k, dq_out, dk_out, q_gain, k_gain, cos,
+                  sin, positions, dq, dk)
     p = _qk_params(q, k, q_gain, k_gain, cos, sin, positions, eps, interleaved)
-    dq = torch.empty(q.shape, dtype=q.dtype, device=q.device) if dq is None else dq
-    dk = torch.empty(k.shape, dtype=k.dtype, device=k.device) if dk is None else dk
+    if dq_out.shape != q.shape or dk_out.shape != k.shape or dq_out.dtype != q.dtype or dk_out.dtype != k.dtype:
+        raise ValueError("dq_out and dk_out must have the shapes and dtype of q and k")
+    dq, dk = _like("dq", dq, q), _like("dk", dk, k)
     dim = q.shape[-1]
     dq_gain = None if q_gain is None else torch.empty(dim, dtype=torch.float32, device=q.device)
     dk_gain = None if k_gain is None else torch.empty(dim, dtype=torch.float32, device=q.device)
     lib = malt.load()
     size = lib.malt_qk_norm_workspace_bytes(dim)
     ws = torch.empty(size, dtype=torch.uint8, device=q.device)
-    _check(lib.malt_qk_norm_backward(p, _heads("dq_out", dq_out, q), _heads("dk_out", dk_out, k), _heads("q", q),
-                                     _heads("k", k), _heads("dq", dq, q), _heads("dk", dk, k), _pointer(dq_gain),
-                                     _pointer(dk_gain), ws.data_ptr(), size,
-                                     _stream(stream, dq, dk, dq_gain, dk_gain, ws)), "malt_qk_norm_backward")
+    _check(lib.malt_qk_norm_backward(p, _heads(dq_out), _heads(dk_out), _heads(q), _heads(k), _heads(dq), _heads(dk),
+                                     _pointer(dq_gain), _pointer(dk_gain), ws.data_ptr(), size,
+                                     _stream(dev, stream, dq, dk, dq_gain, dk_gain, ws)), "malt_qk_norm_backward")
     return dq, dk, dq_gain, dk_gain
 
 
@@ -247,12 +272,8 @@ def _distill_params(logits, top_ids, top_logits, weight, temperature):
                          _float_code("top_logits", top_logits), temperature)
 
 
-def _dlogits(logits, dlogits):
-    if dlogits is None:
-        dlogits = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
-    elif dlogits.shape != logits.shape or dlogits.dtype != logits.dtype:
-        raise ValueError(f"dlogits has shape {tuple(dlogits.shape)} and dtype {dlogits.dtype}, expected those of logits")
-    return dlogits, _row_stride("dlogits", dlogits, logits.shape[-1])
+def _loss(logits):
+    return torch.empty(logits.shape[:-1], dtype=torch.float32, device=logits.device)
 
 
 def distill_loss(logits, top_ids, top_logits, weight=None, temperature: float = 1.0, stream=None):
@@ -262,11 +283,11 @@ def distill_loss(logits, top_ids, top_logits, weight=None, temperature: float = 
     statistics [rows, 2] that distill_grad takes.  Entries with an id outside the
     vocabulary or a logit of -inf are not listed; rows of weight 0 or with nothing
     listed have loss 0."""
-    _on_device(logits=logits, top_ids=top_ids, top_logits=top_logits, weight=weight)
+    dev = _device("logits top_ids top_logits weight", logits, top_ids, top_logits, weight)
     d = _distill_params(logits, top_ids, top_logits, weight, temperature)
-    loss = torch.empty(logits.shape[:-1], dtype=torch.float32, device=logits.device)
+    loss = _loss(logits)
     stats = torch.empty((loss.numel(), 2), dtype=torch.float32, device=logits.device)
-    _check(malt.load().malt_distill_forward(d, loss.data_ptr(), stats.data_ptr(), _stream(stream, loss, stats)),
+    _check(malt.load().malt_distill_forward(d, loss.data_ptr(), stats.data_ptr(), _stream(dev, stream, loss, stats)),
            "malt_distill_forward")
     return loss, stats
 
@@ -275,25 +296,27 @@ def distill_grad(logits, top_ids, top_logits, stats, dloss=None, weight=None, te
                  dlogits=None, stream=None):
     """The gradient of the logits from distill_loss's statistics and the gradient of each row's
     loss (None: ones), in the logits' type; dlogits may be given, also as the logits."""
-    _on_device(logits=logits, top_ids=top_ids, top_logits=top_logits, weight=weight, stats=stats, dloss=dloss,
-               dlogits=dlogits)
+    dev = _device("logits top_ids top_logits weight stats dloss dlogits", logits, top_ids, top_logits, weight, stats,
+                  dloss, dlogits)
     d = _distill_params(logits, top_ids, top_logits, weight, temperature)
     rows = logits.numel() // max(logits.shape[-1], 1)
     _vector("stats", stats, 2 * rows)
     _vector("dloss", dloss, rows)
-    dlogits, ld = _dlogits(logits, dlogits)
+    dlogits = _like("dlogits", dlogits, logits)
+    ld = _row_stride("dlogits", dlogits, logits.shape[-1])
     _check(malt.load().malt_distill_backward(d, stats.data_ptr(), _pointer(dloss), dlogits.data_ptr(), ld,
-                                             _stream(stream, dlogits)), "malt_distill_backward")
+                                             _stream(dev, stream, dlogits)), "malt_distill_backward")
     return dlogits
 
 
 def distill_loss_grad(logits, top_ids, top_logits, weight=None, temperature: float = 1.0, dlogits=None, stream=None):
     """distill_loss and the gradient of the losses' sum in one pass over the logits (a mean is a
     weight of 1 / rows).  Returns (loss, dlogits); dlogits may be given, also as the logits."""
-    _on_device(logits=logits, top_ids=top_ids, top_logits=top_logits, weight=weight, dlogits=dlogits)
+    dev = _device("logits top_ids top_logits weight dlogits", logits, top_ids, top_logits, weight, dlogits)
     d = _distill_params(logits, top_ids, top_logits, weight, temperature)
-    loss = torch.empty(logits.shape[:-1], dtype=torch.float32, device=logits.device)
-    dlogits, ld = _dlogits(logits, dlogits)
+    loss = _loss(logits)
+    dlogits = _like("dlogits", dlogits, logits)
+    ld = _row_stride("dlogits", dlogits, logits.shape[-1])
     _check(malt.load().malt_distill_forward_backward(d, loss.data_ptr(), 0, dlogits.data_ptr(), ld,
-                                                     _stream(stream, loss, dlogits)), "malt_distill_forward_backward")
+                                                     _stream(dev, stream, loss, dlogits)), "malt_distill_forward_backward")
     return loss, dlogits
