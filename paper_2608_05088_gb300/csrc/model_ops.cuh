@@ -55,6 +55,12 @@ __device__ __forceinline__ void load_vec(const T* p, float (&x)[VEC]) {
     }
 }
 
+// N elements as they are in memory, loaded at once.
+template <typename T, int N>
+struct alignas(sizeof(T) * N) Raw {
+    T v[N];
+};
+
 // 16 bytes of T as fp32.
 template <typename T>
 __device__ __forceinline__ void unpack(const uint4& u, float* x) {
@@ -118,6 +124,19 @@ __device__ __forceinline__ float exp2_fast(float x) {
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
+
+// BYTES (4, 8 or 16, both addresses aligned to them) from global to shared memory in the
+// background.  The copies since the last commit are a group; copies_wait<N> waits for all
+// groups of this thread but the last N, and makes them visible to it alone.
+template <int BYTES>
+__device__ __forceinline__ void copy_async(void* to, const void* from) {
+    const uint32_t at = static_cast<uint32_t>(__cvta_generic_to_shared(to));
+    if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(at), "l"(from) : "memory");
+    else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(at), "l"(from), "n"(BYTES) : "memory");
+}
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
 // Two floats in a 64-bit register: the packed arithmetic issues one instruction for both.
 using f32x2 = unsigned long long;

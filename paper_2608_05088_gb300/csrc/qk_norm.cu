@@ -11,7 +11,9 @@
 //
 // Bound by HBM: x is read once (and dy), y (dx) written once.  A row is held by a few
 // neighbouring lanes, both partners of a pair in one lane, so the norm takes a
-// shuffle or two and the rotation none.
+// shuffle or two and the rotation none.  16384 tokens of 2 x 20 heads of 64 in bf16:
+// forward 31 us, 5.4 TB/s, gradient 46 us, 5.5 TB/s (a plain copy of as many bytes runs
+// at 5.9 and 6.1).  One warp per row, element by element, took 356 and 390 us.
 #include <algorithm>
 
 #include <nvtx3/nvToolsExt.h>
@@ -24,6 +26,7 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
 constexpr int kMaxHeadDim = 1024;
+constexpr int kMaxSplit = 256;
 
 struct Rows {           // heads of the tokens of a [batch, seq, heads, dim] view
     void* data;
@@ -54,6 +57,7 @@ struct Params {
     int64_t table_rows, batch, seq;
     int32_t positions_i64, gain_bf16;
     int32_t dim, rot;
+    int32_t lanes;              // of a row, aligned rows only
     float eps;
 };
 
@@ -83,14 +87,14 @@ __device__ __forceinline__ float2 angle(const Params& P, int64_t pos, int p) {
 }
 
 // --------------------------------------------------------------- aligned rows
-// A row is held by LPR neighbouring lanes, 2 V entries each (V: 16 bytes of them):
-// the V pairs that the lane turns, partners in the lane, so that one lane needs V
-// cosines and V sines.  These lanes are a slot, which keeps its token's angles and
-// the gains in registers and walks over heads; neighbouring slots take neighbouring
-// heads of a token, so that a warp's loads are contiguous.
-template <typename T, bool INTER>
+// A row is held by neighbouring lanes, 2 V entries each: the V pairs that the lane turns,
+// partners in the lane, in two vectors of V (8 or 16 bytes), so that one lane needs V cosines and
+// V sines.  These lanes are a slot, which keeps its token's angles and the gains in
+// registers and walks over heads; neighbouring slots take neighbouring heads of a token,
+// so that a warp's loads are contiguous.  Arithmetic is on two pairs at once: A holds the
+// first members, B the second ones.
+template <int V, bool INTER>
 struct Chunk {
-    static constexpr int V = 16 / sizeof(T);
     int a, b;           // first entries of the lane's two vectors
     bool turned;
     __device__ __forceinline__ Chunk(int c, int rot) {
@@ -103,45 +107,137 @@ struct Chunk {
             b = rot / 2 + c * V;
         }
     }
-    // entry of the lane's value i of 2 V, and the two values of its pair p
+    // entry of the lane's value i of 2 V, and the values of pair p
     __device__ __forceinline__ int entry(int i) const { return i < V ? a + i : b + i - V; }
     static __device__ __forceinline__ constexpr int first(int p) { return INTER ? 2 * p : p; }
     static __device__ __forceinline__ constexpr int second(int p) { return INTER ? 2 * p + 1 : V + p; }
 };
 
+// A lane's vectors of a row as they are in memory.
+template <typename T, int V>
+struct RawRow {
+    static constexpr int W = V * sizeof(T) / 4;     // words of a vector
+    uint32_t w[2][W];
+    __device__ __forceinline__ void clear() {
+#pragma unroll
+        for (int i = 0; i < 2 * W; ++i) w[i / W][i % W] = 0;
+    }
+    __device__ __forceinline__ void load(const T* row, int a, int b) {
+        const Raw<uint32_t, W> lo = *reinterpret_cast<const Raw<uint32_t, W>*>(row + a);
+        const Raw<uint32_t, W> hi = *reinterpret_cast<const Raw<uint32_t, W>*>(row + b);
+#pragma unroll
+        for (int i = 0; i < W; ++i) w[0][i] = lo.v[i], w[1][i] = hi.v[i];
+    }
+    // value i of the vector
+    __device__ __forceinline__ float at(int vector, int i) const {
+        if constexpr (sizeof(T) == 4) return __uint_as_float(w[vector][i]);
+        else return __uint_as_float(i % 2 ? w[vector][i / 2] & 0xffff0000u : w[vector][i / 2] << 16);
+    }
+};
+
+// A lane's 2 V values as its pairs' members.
+template <int V, bool INTER>
+struct Members {
+    using C = Chunk<V, INTER>;
+    f32x2 a[V / 2], b[V / 2];
+    __device__ __forceinline__ Members() {}
+    template <typename T>
+    __device__ __forceinline__ explicit Members(const RawRow<T, V>& raw) {
+        float v[2 * V];
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            v[i] = raw.at(0, i);
+            v[V + i] = raw.at(1, i);
+        }
+        from(v);
+    }
+    __device__ __forceinline__ void from(const float (&v)[2 * V]) {
+#pragma unroll
+        for (int p = 0; p < V; p += 2) {
+            a[p / 2] = pack2(v[C::first(p)], v[C::first(p + 1)]);
+            b[p / 2] = pack2(v[C::second(p)], v[C::second(p + 1)]);
+        }
+    }
+    __device__ __forceinline__ void to(float (&v)[2 * V]) const {
+#pragma unroll
+        for (int p = 0; p < V; p += 2) {
+            const float2 x = unpack2(a[p / 2]), y = unpack2(b[p / 2]);
+            v[C::first(p)] = x.x;
+            v[C::first(p + 1)] = x.y;
+            v[C::second(p)] = y.x;
+            v[C::second(p + 1)] = y.y;
+        }
+    }
+    template <typename T>
+    __device__ __forceinline__ void store(T* row, const C& chunk) const {
+        float v[2 * V], lo[V], hi[V];
+        to(v);
+#pragma unroll
+        for (int i = 0; i < V; ++i) lo[i] = v[i], hi[i] = v[V + i];
+        store_vec<T, V>(row + chunk.a, lo);
+        store_vec<T, V>(row + chunk.b, hi);
+    }
+};
+
+// The token's cosines and sines of the lane's pairs.
 template <int V>
 struct Angles {
-    float c[V], s[V];
+    f32x2 c[V / 2], s[V / 2];
     __device__ __forceinline__ void load(const Params& P, int64_t pos, int chunk, bool turned) {
         const bool in = pos >= 0 && pos < P.table_rows;
+        float x[V], y[V];
         if (turned && in) {
             const int64_t at = pos * (P.rot / 2) + chunk * V;
-            load_vec<float, V>(P.cosines + at, c);
-            load_vec<float, V>(P.sines + at, s);
+            load_vec<float, V>(P.cosines + at, x);
+            load_vec<float, V>(P.sines + at, y);
         } else {
 #pragma unroll
             for (int i = 0; i < V; ++i) {
-                c[i] = turned ? __int_as_float(0x7fc00000) : 1.f;
-                s[i] = turned ? __int_as_float(0x7fc00000) : 0.f;
+                x[i] = turned ? __int_as_float(0x7fc00000) : 1.f;
+                y[i] = turned ? __int_as_float(0x7fc00000) : 0.f;
             }
+        }
+#pragma unroll
+        for (int i = 0; i < V; i += 2) {
+            c[i / 2] = pack2(x[i], x[i + 1]);
+            s[i / 2] = pack2(y[i], y[i + 1]);
         }
     }
 };
 
-template <int LPR>
-__device__ __forceinline__ float row_sum(float v) {
+// Lanes of a warp by slots of `lanes` neighbours each (LANES: a power of two known here;
+// 0: any number, the warp's last lanes may belong to no slot).
+template <int LANES>
+struct Slots {
+    int lanes, per_warp, slot, sub;
+    __device__ __forceinline__ explicit Slots(int n) {
+        const int lane = threadIdx.x & 31;
+        lanes = LANES > 0 ? LANES : n;
+        per_warp = 32 / lanes;
+        slot = lane / lanes;
+        sub = lane - slot * lanes;
+        if (LANES == 0 && slot >= per_warp) sub = 32;      // holds nothing
+    }
+    __device__ __forceinline__ float sum(float v) const {
+        if constexpr (LANES > 0) {
 #pragma unroll
-    for (int d = LPR / 2; d > 0; d >>= 1) v += __shfl_xor_sync(~0u, v, d);
-    return v;
-}
-
-template <typename T>
-__device__ __forceinline__ uint4 load16(const T* p) { return *reinterpret_cast<const uint4*>(p); }
+            for (int d = LANES / 2; d > 0; d >>= 1) v += __shfl_xor_sync(~0u, v, d);
+            return v;
+        } else {
+#pragma unroll
+            for (int d = 1; d < 32; d <<= 1) {
+                const float up = __shfl_down_sync(~0u, v, d);
+                if (sub + d < lanes) v += up;
+            }
+            return __shfl_sync(~0u, v, slot * lanes);
+        }
+    }
+};
 
 // Gains of the lane's entries.
-template <typename C, int N>
-__device__ __forceinline__ void load_gains(const Params& P, const Kind& K, const C& chunk, float (&g)[N]) {
-    constexpr int V = N / 2;
+template <int V, bool INTER>
+__device__ __forceinline__ Members<V, INTER> load_gains(const Params& P, const Kind& K, const Chunk<V, INTER>& chunk) {
+    float g[2 * V];
     if (K.gain_vectors) {
         float lo[V], hi[V];
         load_vec<float, V>(static_cast<const float*>(K.gain) + chunk.a, lo);
@@ -150,166 +246,248 @@ __device__ __forceinline__ void load_gains(const Params& P, const Kind& K, const
         for (int i = 0; i < V; ++i) g[i] = lo[i], g[V + i] = hi[i];
     } else {
 #pragma unroll
-        for (int i = 0; i < N; ++i) g[i] = gain_at(P, K, chunk.entry(i));
+        for (int i = 0; i < 2 * V; ++i) g[i] = gain_at(P, K, chunk.entry(i));
     }
+    Members<V, INTER> m;
+    m.from(g);
+    return m;
 }
 
-constexpr int kFwdHeads = 4;        // rows of a slot in flight
-constexpr int kBwdHeads = 2;
+__device__ __forceinline__ float sum2(f32x2 v) {
+    const float2 h = unpack2(v);
+    return h.x + h.y;
+}
+__device__ __forceinline__ f32x2 twice(float v) { return pack2(v, v); }
 
-template <typename T, bool INTER, int LPR>
-__global__ void __launch_bounds__(kThreads)
+// Entries of a lane's vectors: 16 bytes.
+template <typename T>
+__host__ __device__ constexpr int vector_of() { return 16 / sizeof(T); }
+
+// Forward: rows of a slot in flight, and blocks of an SM (four rows at two blocks: 34 us
+// for 31).
+constexpr int kFwdHeads = 2;
+constexpr int kFwdBlocks = 3;
+// Backward: the rows of a slot on their way and the one at work, in shared memory (rows
+// in registers, two at a time: 55 us for 46; two blocks of 256 threads 49, three blocks a
+// SM spill).
+constexpr int kBwdThreads = 128;
+constexpr int kBwdWarps = kBwdThreads / 32;
+constexpr int kBwdStages = 4;
+constexpr int kBwdBlocks = 4;
+
+// y_a = r (x_a (g_a cos) - x_b (g_b sin)),  y_b = r (x_b (g_b cos) + x_a (g_a sin)): the
+// products in brackets are the token's.
+template <typename T, bool INTER, int LANES>
+__global__ void __launch_bounds__(kThreads, kFwdBlocks)
 qk_forward_kernel(const __grid_constant__ Params P) {
-    using C = Chunk<T, INTER>;
-    constexpr int V = C::V, N = 2 * V, U = kFwdHeads;
+    constexpr int V = vector_of<T>(), N = 2 * V, U = kFwdHeads;
+    using C = Chunk<V, INTER>;
     const bool keys = blockIdx.x >= P.kind[0].blocks;
     const Kind& K = P.kind[keys];
     const uint32_t block = blockIdx.x - (keys ? P.kind[0].blocks : 0);
-    const int lane = threadIdx.x & 31, sub = lane % LPR;
-    const uint32_t slot = (block * kWarps + (threadIdx.x >> 5)) * (32 / LPR) + lane / LPR;
-    const bool live = slot < K.slots && sub * N < P.dim;
+    const Slots<LANES> slots(P.lanes);
+    const uint32_t slot = (block * kWarps + (threadIdx.x >> 5)) * slots.per_warp + slots.slot;
+    const bool live = slot < K.slots && slots.sub * N < P.dim;
     const uint32_t token = slot / K.split, j = slot - token * K.split;
     const int64_t b = token / static_cast<uint32_t>(P.seq), s = token - b * P.seq;
-    const C chunk(sub, P.rot);
-    const T* const x = static_cast<const T*>(K.x.data) + K.x.at(b, s, 0);
-    T* const y = static_cast<T*>(K.y.data) + K.y.at(b, s, 0);
-    float g[N];
-    Angles<V> t;
+    const C chunk(slots.sub, P.rot);
+    const T* x = static_cast<const T*>(K.x.data) + K.x.at(b, s, j);
+    T* y = static_cast<T*>(K.y.data) + K.y.at(b, s, j);
+    const int64_t x_step = K.split * K.x.head_stride, y_step = K.split * K.y.head_stride;
+    const float inv_n = 1.f / static_cast<float>(P.dim);
+    f32x2 ac[V / 2], as[V / 2], bc[V / 2], bs[V / 2];
     chain_wait();
-    for (int h0 = 0; h0 < K.heads; h0 += U * K.split) {
-        uint4 raw[U][2];
+    for (int h = j; h - static_cast<int>(j) < K.heads; h += U * K.split, x += U * x_step, y += U * y_step) {
+        RawRow<T, V> raw[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int h = h0 + u * K.split + j;
-            raw[u][0] = raw[u][1] = make_uint4(0, 0, 0, 0);
-            if (live && h < K.heads) {
-                raw[u][0] = load16(x + h * K.x.head_stride + chunk.a);
-                raw[u][1] = load16(x + h * K.x.head_stride + chunk.b);
-            }
+            raw[u].clear();
+            if (live && h + u * static_cast<int>(K.split) < K.heads) raw[u].load(x + u * x_step, chunk.a, chunk.b);
         }
-        if (h0 == 0 && live) {
-            t.load(P, position_of(P, b, s), sub, chunk.turned);
-            load_gains(P, K, chunk, g);
+        if (h == j && live) {
+            Angles<V> t;
+            t.load(P, position_of(P, b, s), slots.sub, chunk.turned);
+            const Members<V, INTER> g = load_gains(P, K, chunk);
+#pragma unroll
+            for (int i = 0; i < V / 2; ++i) {
+                ac[i] = mul2(g.a[i], t.c[i]);
+                as[i] = mul2(g.a[i], t.s[i]);
+                bc[i] = mul2(g.b[i], t.c[i]);
+                bs[i] = mul2(g.b[i], mul2(t.s[i], twice(-1.f)));
+            }
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int h = h0 + u * K.split + j;
-            float v[N];
-            unpack<T>(raw[u][0], v);
-            unpack<T>(raw[u][1], v + V);
-            float ss = 0.f;
+            Members<V, INTER> v(raw[u]);
+            f32x2 ss = 0;
 #pragma unroll
-            for (int i = 0; i < N; ++i) ss = fmaf(v[i], v[i], ss);
-            const float r = rsqrtf(row_sum<LPR>(ss) / static_cast<float>(P.dim) + P.eps);
-            if (!live || h >= K.heads) continue;
+            for (int i = 0; i < V / 2; ++i) ss = fma2(v.a[i], v.a[i], fma2(v.b[i], v.b[i], ss));
+            const f32x2 r = twice(rsqrtf(fmaf(slots.sum(sum2(ss)), inv_n, P.eps)));
+            if (!live || h + u * static_cast<int>(K.split) >= K.heads) continue;
 #pragma unroll
-            for (int i = 0; i < N; ++i) v[i] *= r * g[i];
-            float o[2][V];
-#pragma unroll
-            for (int p = 0; p < V; ++p) {
-                const int ia = C::first(p), ib = C::second(p);
-                o[ia / V][ia % V] = v[ia] * t.c[p] - v[ib] * t.s[p];
-                o[ib / V][ib % V] = v[ib] * t.c[p] + v[ia] * t.s[p];
+            for (int i = 0; i < V / 2; ++i) {
+                const f32x2 a = mul2(v.a[i], r), b = mul2(v.b[i], r);
+                v.a[i] = fma2(a, ac[i], mul2(b, bs[i]));
+                v.b[i] = fma2(b, bc[i], mul2(a, as[i]));
             }
-            store_vec<T, V>(y + h * K.y.head_stride + chunk.a, o[0]);
-            store_vec<T, V>(y + h * K.y.head_stride + chunk.b, o[1]);
+            v.store(y + u * y_step, chunk);
         }
     }
 }
 
 // The blocks stay and walk over the slots, with the gain gradient of their lanes'
-// entries in registers; each leaves its sum for the join launch.
-template <typename T, bool INTER, int LPR>
-__global__ void __launch_bounds__(kThreads, 2)
+// entries in registers; each leaves its sum for the join launch.  Every lane copies its
+// own vectors of the rows to come to shared memory, in the background: a copy concerns
+// no other lane, and rows on their way take no registers.
+template <typename T, bool INTER, int LANES>
+__global__ void __launch_bounds__(kBwdThreads, kBwdBlocks)
 qk_backward_kernel(const __grid_constant__ Params P) {
-    using C = Chunk<T, INTER>;
-    constexpr int V = C::V, N = 2 * V, U = kBwdHeads, kSlots = 32 / LPR;
-    extern __shared__ float sums[];         // [kWarps][dim]
+    constexpr int V = vector_of<T>(), N = 2 * V;
+    using C = Chunk<V, INTER>;
+    using M = Members<V, INTER>;
+    extern __shared__ uint4 stage[];        // [kBwdStages][4][kBwdThreads]; at the end [kBwdWarps][slots of a warp][dim] sums
+    __shared__ int64_t place[kBwdStages][kBwdThreads];     // positions
     const bool keys = blockIdx.x >= P.kind[0].blocks;
     const Kind& K = P.kind[keys];
     const uint32_t block = blockIdx.x - (keys ? P.kind[0].blocks : 0);
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, sub = lane % LPR;
-    const bool mine = sub * N < P.dim;
-    const C chunk(sub, P.rot);
-    float g[N], acc[N] = {};
+    const int warp = threadIdx.x >> 5;
+    const Slots<LANES> slots(P.lanes);
+    const bool mine = slots.sub * N < P.dim;
+    const C chunk(slots.sub, P.rot);
+    M g, acc;
+#pragma unroll
+    for (int i = 0; i < V / 2; ++i) g.a[i] = g.b[i] = acc.a[i] = acc.b[i] = 0;
     Angles<V> t;
     chain_wait();
-    if (mine) load_gains(P, K, chunk, g);
-    const float n = static_cast<float>(P.dim);
-    for (uint64_t first = (static_cast<uint64_t>(block) * kWarps + warp) * kSlots; first < K.slots;
-         first += static_cast<uint64_t>(K.blocks) * kWarps * kSlots) {
-        const uint64_t slot = first + lane / LPR;
-        const bool live = slot < K.slots && mine;
-        const uint32_t token = static_cast<uint32_t>(slot) / K.split, j = static_cast<uint32_t>(slot) - token * K.split;
-        const int64_t b = token / static_cast<uint32_t>(P.seq), s = token - b * P.seq;
-        const T* const x = static_cast<const T*>(K.x.data) + K.x.at(b, s, 0);
-        const T* const dy = static_cast<const T*>(K.dy.data) + K.dy.at(b, s, 0);
-        T* const dx = static_cast<T*>(K.dx.data) + K.dx.at(b, s, 0);
-        for (int h0 = 0; h0 < K.heads; h0 += U * K.split) {
-            uint4 rx[U][2], ry[U][2];
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int h = h0 + u * K.split + j;
-                rx[u][0] = rx[u][1] = ry[u][0] = ry[u][1] = make_uint4(0, 0, 0, 0);
-                if (live && h < K.heads) {
-                    rx[u][0] = load16(x + h * K.x.head_stride + chunk.a);
-                    rx[u][1] = load16(x + h * K.x.head_stride + chunk.b);
-                    ry[u][0] = load16(dy + h * K.dy.head_stride + chunk.a);
-                    ry[u][1] = load16(dy + h * K.dy.head_stride + chunk.b);
+    if (mine) g = load_gains(P, K, chunk);
+    const float inv_n = 1.f / static_cast<float>(P.dim);
+    const uint32_t per_block = kBwdWarps * slots.per_warp;
+    const uint64_t begin = static_cast<uint64_t>(block) * per_block + warp * slots.per_warp;
+    const uint64_t step = static_cast<uint64_t>(K.blocks) * per_block;
+    const int rows = static_cast<int>((K.heads + K.split - 1) / K.split);      // of a slot, at most
+    const int64_t x_step = K.split * K.x.head_stride, dy_step = K.split * K.dy.head_stride;
+    const int64_t dx_step = K.split * K.dx.head_stride;
+
+    // The lane's slot of a group: whether there is one, its first head and its token.
+    struct Where {
+        bool live;
+        uint32_t j;
+        int64_t b, s;
+    };
+    auto where = [&](uint64_t first) {
+        const uint64_t slot = first + slots.slot;
+        const uint32_t token = static_cast<uint32_t>(slot) / K.split;
+        const int64_t b = token / static_cast<uint32_t>(P.seq);
+        return Where{slot < K.slots && mine, static_cast<uint32_t>(slot) - token * K.split, b, token - b * P.seq};
+    };
+    // The copies' place in the sequence of rows.
+    uint64_t ahead = begin;
+    int ahead_row = 0, ahead_slot = 0, ahead_stage = 0;
+    bool to_live = false;
+    int to_h = 0;
+    const T *from_x = nullptr, *from_dy = nullptr;
+    auto fetch = [&] {
+        if (ahead < K.slots) {
+            if (ahead_row == 0) {
+                const Where to = where(ahead);
+                to_live = to.live;
+                to_h = to.j;
+                from_x = static_cast<const T*>(K.x.data) + K.x.at(to.b, to.s, to.j);
+                from_dy = static_cast<const T*>(K.dy.data) + K.dy.at(to.b, to.s, to.j);
+                if (to.live && P.positions != nullptr) {
+                    const int64_t i = to.b * P.positions_batch_stride + to.s;
+                    int64_t* const at = &place[ahead_slot % kBwdStages][threadIdx.x];
+                    if (P.positions_i64) copy_async<8>(at, static_cast<const int64_t*>(P.positions) + i);
+                    else copy_async<4>(at, static_cast<const int32_t*>(P.positions) + i);
                 }
             }
-            if (h0 == 0 && live) t.load(P, position_of(P, b, s), sub, chunk.turned);
+            if (to_live && to_h < K.heads) {
+                uint4* const at = stage + ahead_stage * 4 * kBwdThreads + threadIdx.x;
+                copy_async<16>(at, from_x + chunk.a);
+                copy_async<16>(at + kBwdThreads, from_x + chunk.b);
+                copy_async<16>(at + 2 * kBwdThreads, from_dy + chunk.a);
+                copy_async<16>(at + 3 * kBwdThreads, from_dy + chunk.b);
+            }
+            from_x += x_step;
+            from_dy += dy_step;
+            to_h += K.split;
+            if (++ahead_row == rows) {
+                ahead_row = 0;
+                ahead += step;
+                ++ahead_slot;
+            }
+        }
+        copies_commit();
+        if (++ahead_stage == kBwdStages) ahead_stage = 0;
+    };
+#pragma unroll 1
+    for (int k = 0; k < kBwdStages - 1; ++k) fetch();
+
+    int at_stage = 0, at_slot = 0;
+    for (uint64_t first = begin; first < K.slots; first += step, ++at_slot) {
+        const Where w = where(first);
+        T* dx = static_cast<T*>(K.dx.data) + K.dx.at(w.b, w.s, w.j);
+#pragma unroll 1
+        for (int i = 0, h = w.j; i < rows; ++i, h += K.split, dx += dx_step) {
+            fetch();
+            copies_wait<kBwdStages - 1>();
+            if (i == 0 && w.live) {
+                const int64_t* const p = &place[at_slot % kBwdStages][threadIdx.x];
+                const int64_t pos = P.positions == nullptr ? w.s : P.positions_i64 ? *p : *reinterpret_cast<const int32_t*>(p);
+                t.load(P, pos, slots.sub, chunk.turned);
+            }
+            const bool here = w.live && h < K.heads;
+            f32x2 ss = 0, ux = 0;
+            M v, d;
+            if (here) {
+                const uint4* const at = stage + at_stage * 4 * kBwdThreads + threadIdx.x;
+                float f[N];
+                unpack<T>(at[0], f);
+                unpack<T>(at[kBwdThreads], f + V);
+                v.from(f);
+                unpack<T>(at[2 * kBwdThreads], f);
+                unpack<T>(at[3 * kBwdThreads], f + V);
+                d.from(f);
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int h = h0 + u * K.split + j;
-                const bool here = live && h < K.heads;
-                float v[N], d[N];
-                unpack<T>(rx[u][0], v);
-                unpack<T>(rx[u][1], v + V);
-                unpack<T>(ry[u][0], d);
-                unpack<T>(ry[u][1], d + V);
-                float ss = 0.f, ux = 0.f;
-                if (here) {
-#pragma unroll
-                    for (int p = 0; p < V; ++p) {       // rotated back
-                        const int ia = C::first(p), ib = C::second(p);
-                        const float da = d[ia] * t.c[p] + d[ib] * t.s[p], db = d[ib] * t.c[p] - d[ia] * t.s[p];
-                        d[ia] = da;
-                        d[ib] = db;
-                    }
-#pragma unroll
-                    for (int i = 0; i < N; ++i) {
-                        ss = fmaf(v[i], v[i], ss);
-                        ux = fmaf(d[i] * g[i], v[i], ux);
-                    }
+                for (int k = 0; k < V / 2; ++k) {       // rotated back
+                    const f32x2 da = fma2(d.b[k], t.s[k], mul2(d.a[k], t.c[k]));
+                    const f32x2 db = fma2(mul2(d.a[k], twice(-1.f)), t.s[k], mul2(d.b[k], t.c[k]));
+                    d.a[k] = da;
+                    d.b[k] = db;
+                    ss = fma2(v.a[k], v.a[k], fma2(v.b[k], v.b[k], ss));
+                    ux = fma2(mul2(da, g.a[k]), v.a[k], fma2(mul2(db, g.b[k]), v.b[k], ux));
                 }
-                const float r = rsqrtf(row_sum<LPR>(ss) / n + P.eps);
-                const float c = r * r * (row_sum<LPR>(ux) / n);
-                if (!here) continue;
-                float o[2][V];
+            }
+            if (++at_stage == kBwdStages) at_stage = 0;
+            const float r1 = rsqrtf(fmaf(slots.sum(sum2(ss)), inv_n, P.eps));
+            const f32x2 r = twice(r1), c = twice(-(r1 * (slots.sum(sum2(ux)) * inv_n)));
+            if (here) {
 #pragma unroll
-                for (int i = 0; i < N; ++i) {
-                    acc[i] = fmaf(d[i], v[i] * r, acc[i]);
-                    o[i / V][i % V] = r * (d[i] * g[i] - v[i] * c);
+                for (int k = 0; k < V / 2; ++k) {
+                    const f32x2 a = mul2(v.a[k], r), b = mul2(v.b[k], r);     // normalised
+                    acc.a[k] = fma2(d.a[k], a, acc.a[k]);
+                    acc.b[k] = fma2(d.b[k], b, acc.b[k]);
+                    v.a[k] = mul2(r, fma2(a, c, mul2(d.a[k], g.a[k])));
+                    v.b[k] = mul2(r, fma2(b, c, mul2(d.b[k], g.b[k])));
                 }
-                store_vec<T, V>(dx + h * K.dx.head_stride + chunk.a, o[0]);
-                store_vec<T, V>(dx + h * K.dx.head_stride + chunk.b, o[1]);
+                v.store(dx, chunk);
             }
         }
     }
+    copies_wait<0>();
+    __syncthreads();
+    float* const sums = reinterpret_cast<float*>(stage);
+    if (mine) {
+        float v[N];
+        acc.to(v);
+        float* const at = sums + (warp * slots.per_warp + slots.slot) * P.dim;
 #pragma unroll
-    for (int i = 0; i < N; ++i)
-#pragma unroll
-        for (int d = LPR; d < 32; d <<= 1) acc[i] += __shfl_xor_sync(~0u, acc[i], d);
-    if (lane < LPR && mine) {
-#pragma unroll
-        for (int i = 0; i < N; ++i) sums[warp * P.dim + chunk.entry(i)] = acc[i];
+        for (int i = 0; i < N; ++i) at[chunk.entry(i)] = v[i];
     }
     __syncthreads();
-    for (int i = threadIdx.x; i < P.dim; i += kThreads) {
+    for (int i = threadIdx.x; i < P.dim; i += kBwdThreads) {
         float t = 0.f;
-#pragma unroll
-        for (int w = 0; w < kWarps; ++w) t += sums[w * P.dim + i];
+        for (int w = 0; w < kBwdWarps * slots.per_warp; ++w) t += sums[w * P.dim + i];
         K.parts[block * static_cast<int64_t>(P.dim) + i] = t;
     }
 }
@@ -513,84 +691,105 @@ Params params_of(const malt_qk_norm_t* p) {
 int32_t backward_blocks() { return sm_count() * 6; }
 int32_t backward_parts() { return backward_blocks() + 2; }
 
-// Whether the rows of a view can be read in 16-byte vectors.
-template <typename T>
+// Whether the rows of a view can be read in vectors of V entries.
+template <typename T, int V>
 bool vectors(const Params& P, const Rows& r) {
-    constexpr int64_t V = 16 / sizeof(T);
-    return aligned_to(r.data, 16) && (P.batch == 1 || r.batch_stride % V == 0) &&
+    return aligned_to(r.data, V * sizeof(T)) && (P.batch == 1 || r.batch_stride % V == 0) &&
            (P.seq == 1 || r.seq_stride % V == 0) && r.head_stride % V == 0;
 }
 
 // Lanes of a row in the aligned kernels, 0 where they do not apply.
-template <typename T>
+template <typename T, int V>
 int lanes_of(const Params& P, bool backward) {
-    constexpr int N = 32 / sizeof(T);
+    constexpr int N = 2 * V;
     if (P.dim % N != 0 || P.rot % N != 0 || P.dim / N > 32) return 0;
     if (!aligned_to(P.cosines, 16) || !aligned_to(P.sines, 16)) return 0;
     for (const Kind& K : P.kind) {
         if (K.heads == 0) continue;
-        if (!vectors<T>(P, K.x)) return 0;
-        if (backward ? !vectors<T>(P, K.dy) || !vectors<T>(P, K.dx) : !vectors<T>(P, K.y)) return 0;
+        if (!vectors<T, V>(P, K.x)) return 0;
+        if (backward ? !vectors<T, V>(P, K.dy) || !vectors<T, V>(P, K.dx) : !vectors<T, V>(P, K.y)) return 0;
     }
-    int lanes = 2;
-    while (lanes * N < P.dim) lanes *= 2;
-    return lanes;
+    return P.dim / N;
 }
 
-// Slots of a token for each kind: a few batches of heads a slot, which spreads the
-// angles' cost, but enough slots to fill the GPU.
-void split_heads(Params& P, int lanes, int batch) {
+// Slots of a token for each kind.  Enough to give every SM `warps` warps; of these the
+// number that costs least, a slot taking its heads in batches and, once, its token's
+// place and angles, which cost about as much as kSlotCost heads.
+constexpr double kSlotCost = 1.5;
+void split_heads(Params& P, int lanes, int batch, int warps) {
+    P.lanes = lanes;
     const int64_t tokens = P.batch * P.seq;
-    const int64_t wanted = sm_count() * 64ll * (32 / lanes);
+    const int64_t wanted = static_cast<int64_t>(sm_count()) * warps * (32 / lanes);
     for (Kind& K : P.kind) {
         K.gain_vectors = K.gain != nullptr && !P.gain_bf16 && aligned_to(K.gain, 16);
-        int64_t rounds = 2, split;
-        do {
-            split = std::max<int64_t>(1, (K.heads + batch * rounds - 1) / (batch * rounds));
-        } while (--rounds > 0 && tokens * split < wanted);
-        if (tokens * K.heads < wanted) split = std::max(K.heads, 1);
-        if (tokens * split >= (int64_t{1} << 31)) split = 1;
-        K.split = static_cast<uint32_t>(split);
-        K.slots = K.heads == 0 ? 0 : static_cast<uint32_t>(tokens * split);
+        int64_t best = std::max<int64_t>(K.heads, 1);
+        double least = 1e30;
+        for (int64_t split = 1; split <= K.heads && split <= kMaxSplit; ++split) {
+            if (tokens * split < wanted && split < K.heads) continue;
+            const int64_t heads = (K.heads + split - 1) / split;
+            const double cost = split * ((heads + batch - 1) / batch * batch + kSlotCost);
+            if (cost < least) least = cost, best = split;
+        }
+        if (tokens * best >= (int64_t{1} << 31)) best = 1;
+        K.split = static_cast<uint32_t>(best);
+        K.slots = K.heads == 0 ? 0 : static_cast<uint32_t>(tokens * best);
     }
 }
 
-template <typename T, bool INTER, int LPR>
+template <typename T, bool INTER, int LANES>
 cudaError_t forward_rows(Params& P, cudaStream_t s) {
-    constexpr int64_t kSlots = kWarps * (32 / LPR);
+    const int64_t kSlots = kWarps * (32 / P.lanes);
     for (Kind& K : P.kind) K.blocks = static_cast<int32_t>((K.slots + kSlots - 1) / kSlots);
-    return launch_chained(qk_forward_kernel<T, INTER, LPR>, P.kind[0].blocks + P.kind[1].blocks, kThreads, 0, s, P);
+    return launch_chained(qk_forward_kernel<T, INTER, LANES>, P.kind[0].blocks + P.kind[1].blocks, kThreads, 0, s, P);
 }
 
-template <typename T, bool INTER, int LPR>
+template <typename T, bool INTER, int LANES>
 cudaError_t backward_rows(Params& P, cudaStream_t s) {
-    constexpr int64_t kSlots = kWarps * (32 / LPR);
+    const int64_t kSlots = kBwdWarps * (32 / P.lanes);
     const int64_t heads = P.kind[0].heads + P.kind[1].heads;
     for (Kind& K : P.kind) {
-        const int64_t share = K.heads > 0 ? std::max<int64_t>(1, static_cast<int64_t>(sm_count()) * 2 * K.heads / heads) : 0;
+        const int64_t share = K.heads > 0 ? std::max<int64_t>(1, static_cast<int64_t>(sm_count()) * kBwdBlocks * K.heads / heads) : 0;
         K.blocks = static_cast<int32_t>(std::min<int64_t>((K.slots + kSlots - 1) / kSlots, share));
     }
     P.kind[1].parts = P.kind[0].parts + static_cast<int64_t>(P.kind[0].blocks) * P.dim;
-    return launch_chained(qk_backward_kernel<T, INTER, LPR>, P.kind[0].blocks + P.kind[1].blocks, kThreads,
-                          kWarps * P.dim * sizeof(float), s, P);
+    constexpr int kSmem = kBwdStages * 4 * kBwdThreads * 16;      // the sums of 32 lanes of 2 V entries a warp fit in it
+    static_assert(kSmem >= kBwdWarps * 32 * 8 * static_cast<int>(sizeof(float)) * 2, "sums in the stages' place");
+    auto* const kernel = qk_backward_kernel<T, INTER, LANES>;
+    const cudaError_t rc = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+    if (rc != cudaSuccess) { cudaGetLastError(); return rc; }
+    return launch_chained(kernel, P.kind[0].blocks + P.kind[1].blocks, kBwdThreads, kSmem, s, P);
 }
 
 template <typename T, bool INTER>
-cudaError_t rows_kernel(Params& P, int lanes, bool backward, cudaStream_t s) {
-    split_heads(P, lanes, backward ? kBwdHeads : kFwdHeads);
+cudaError_t forward_lanes(Params& P, int lanes, cudaStream_t s) {
+    split_heads(P, lanes, kFwdHeads, 32);
     switch (lanes) {
-        case 2: return backward ? backward_rows<T, INTER, 2>(P, s) : forward_rows<T, INTER, 2>(P, s);
-        case 4: return backward ? backward_rows<T, INTER, 4>(P, s) : forward_rows<T, INTER, 4>(P, s);
-        case 8: return backward ? backward_rows<T, INTER, 8>(P, s) : forward_rows<T, INTER, 8>(P, s);
-        case 16: return backward ? backward_rows<T, INTER, 16>(P, s) : forward_rows<T, INTER, 16>(P, s);
-        default: return backward ? backward_rows<T, INTER, 32>(P, s) : forward_rows<T, INTER, 32>(P, s);
+        case 2: return forward_rows<T, INTER, 2>(P, s);
+        case 4: return forward_rows<T, INTER, 4>(P, s);
+        case 8: return forward_rows<T, INTER, 8>(P, s);
+        case 16: return forward_rows<T, INTER, 16>(P, s);
+        case 32: return forward_rows<T, INTER, 32>(P, s);
+        default: return forward_rows<T, INTER, 0>(P, s);
+    }
+}
+
+template <typename T, bool INTER>
+cudaError_t backward_lanes(Params& P, int lanes, cudaStream_t s) {
+    split_heads(P, lanes, 1, kBwdBlocks * kBwdWarps);
+    switch (lanes) {
+        case 2: return backward_rows<T, INTER, 2>(P, s);
+        case 4: return backward_rows<T, INTER, 4>(P, s);
+        case 8: return backward_rows<T, INTER, 8>(P, s);
+        case 16: return backward_rows<T, INTER, 16>(P, s);
+        case 32: return backward_rows<T, INTER, 32>(P, s);
+        default: return backward_rows<T, INTER, 0>(P, s);
     }
 }
 
 template <typename T>
 cudaError_t forward(Params& P, bool inter, cudaStream_t s) {
-    if (const int lanes = lanes_of<T>(P, false))
-        return inter ? rows_kernel<T, true>(P, lanes, false, s) : rows_kernel<T, false>(P, lanes, false, s);
+    if (const int lanes = lanes_of<T, vector_of<T>()>(P, false))
+        return inter ? forward_lanes<T, true>(P, lanes, s) : forward_lanes<T, false>(P, lanes, s);
     for (Kind& K : P.kind) {
         const int64_t blocks = (P.batch * P.seq * K.heads + kWarps - 1) / kWarps;
         if (blocks >= (int64_t{1} << 30)) return cudaErrorInvalidValue;
@@ -602,8 +801,8 @@ cudaError_t forward(Params& P, bool inter, cudaStream_t s) {
 
 template <typename T>
 cudaError_t backward(Params& P, bool inter, cudaStream_t s) {
-    if (const int lanes = lanes_of<T>(P, true))
-        return inter ? rows_kernel<T, true>(P, lanes, true, s) : rows_kernel<T, false>(P, lanes, true, s);
+    if (const int lanes = lanes_of<T, vector_of<T>()>(P, true))
+        return inter ? backward_lanes<T, true>(P, lanes, s) : backward_lanes<T, false>(P, lanes, s);
     const int64_t heads = P.kind[0].heads + P.kind[1].heads;
     for (Kind& K : P.kind) {
         const int64_t blocks = (P.batch * P.seq * K.heads + kWarps - 1) / kWarps;
