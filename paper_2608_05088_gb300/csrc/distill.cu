@@ -193,7 +193,8 @@ __device__ __forceinline__ void list_entries(const Params& P, int64_t row, const
         float t[1] = {-INFINITY};
         if (j < P.top) {
             const int64_t id_at = row * P.top_ids_ld + j, at = row * P.top_logits_ld + j;
-            id = P.ids_i64 ? static_cast<const int64_t*>(P.top_ids)[id_at] : static_cast<const int32_t*>(P.top_ids)[id_at];
+            id = P.ids_i64 ? static_cast<const int64_t*>(P.top_ids)[id_at]
+                           : static_cast<const int32_t*>(P.top_ids)[id_at];
             if (P.top_bf16) load_vec<bf16, 1>(static_cast<const bf16*>(P.top_logits) + at, t);
             else load_vec<float, 1>(static_cast<const float*>(P.top_logits) + at, t);
         }
@@ -261,8 +262,10 @@ template <typename T, bool SAME, int VEC>
 __device__ __forceinline__ void put(T* at, const float (&v)[VEC]) {
     if constexpr (SAME) {
         uint4 u;
-        if constexpr (sizeof(T) == 4) u = make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
-        else u = make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
+        if constexpr (sizeof(T) == 4)
+            u = make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
+        else
+            u = make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
         __stcs(reinterpret_cast<uint4*>(at), u);
     } else {
 #pragma unroll
@@ -348,7 +351,8 @@ struct Part {
     __device__ __forceinline__ Part(const T* x, int vocab, int part, int shift, bool sweeps) {
         // Vectors start on 16-byte addresses: `lead` entries come before the first one.
         const int parts = 1 << shift;
-        const int lead = min(vocab, static_cast<int>(-(static_cast<uint32_t>(reinterpret_cast<uintptr_t>(x)) / sizeof(T)) % VEC));
+        const int past = static_cast<int>(reinterpret_cast<uintptr_t>(x) % 16 / sizeof(T));
+        const int lead = min(vocab, (VEC - past) % VEC);
         const int vectors = (vocab - lead) / VEC;
         const int v_begin = static_cast<int>(static_cast<int64_t>(vectors) * part >> shift);
         const int v_end = static_cast<int>(static_cast<int64_t>(vectors) * (part + 1) >> shift);
@@ -410,7 +414,8 @@ distill_kernel(const __grid_constant__ Params P) {
         const T* const at = xv + static_cast<int64_t>(i) * VEC;
 #pragma unroll
         for (int k = 0; k < kBatch; ++k)
-            u[k] = i + k * N < count ? *reinterpret_cast<const uint4*>(at + k * N * VEC) : make_uint4(kNone, kNone, kNone, kNone);
+            u[k] = i + k * N < count ? *reinterpret_cast<const uint4*>(at + k * N * VEC)
+                                     : make_uint4(kNone, kNone, kNone, kNone);
     };
     if (!teacher) load(threadIdx.x);
     if (teacher) {
@@ -442,7 +447,8 @@ distill_kernel(const __grid_constant__ Params P) {
         if (GRAD) {
             const float zero[VEC] = {}, none[1] = {};
             if (odd >= 0) store_vec<T, 1>(dx + odd, none);
-            for (int i = threadIdx.x; i < count; i += kAll) put<T, SAME, VEC>(dxv + static_cast<int64_t>(i) * VEC, zero);
+            for (int i = threadIdx.x; i < count; i += kAll)
+                put<T, SAME, VEC>(dxv + static_cast<int64_t>(i) * VEC, zero);
         }
         return;
     }
@@ -482,7 +488,8 @@ int check(const malt_distill_t* d) {
         !(d->temperature <= 1e15f))
         return MALT_ERR_INVALID_ARG;
     if (!float_type(d->dtype) || !float_type(d->top_dtype) || !index_type(d->ids_dtype)) return MALT_ERR_UNSUPPORTED;
-    if (d->top > kMaxTop || d->rows >= (int64_t{1} << 27) || d->vocab >= (int64_t{1} << 31)) return MALT_ERR_UNSUPPORTED;
+    if (d->top > kMaxTop || d->rows >= (int64_t{1} << 27) || d->vocab >= (int64_t{1} << 31))
+        return MALT_ERR_UNSUPPORTED;
     if (d->ld < d->vocab || d->top_ids_ld < d->top || d->top_logits_ld < d->top) return MALT_ERR_INVALID_ARG;
     if (d->rows > 0 && (d->logits == nullptr || (d->top > 0 && (d->top_ids == nullptr || d->top_logits == nullptr))))
         return MALT_ERR_INVALID_ARG;
@@ -498,9 +505,10 @@ int64_t entries_bytes(int64_t top) { return 16 * padded_top(static_cast<int>(top
 template <typename T, bool FWD, bool GRAD, int WIDTH>
 cudaError_t launch_width(const malt_distill_t* d, const Params& P, int parts, cudaStream_t s) {
     constexpr int V = 16 / sizeof(T);
-    const bool same = !GRAD || (reinterpret_cast<uintptr_t>(P.logits) % 16 == reinterpret_cast<uintptr_t>(P.dlogits) % 16 &&
-                                (P.ld - P.dlogits_ld) % V == 0);
-    return launch_clusters(same ? distill_kernel<T, FWD, GRAD, true, WIDTH> : distill_kernel<T, FWD, GRAD, !GRAD, WIDTH>,
+    auto past = [](const void* p) { return reinterpret_cast<uintptr_t>(p) % 16; };
+    const bool same = !GRAD || (past(P.logits) == past(P.dlogits) && (P.ld - P.dlogits_ld) % V == 0);
+    return launch_clusters(same ? distill_kernel<T, FWD, GRAD, true, WIDTH>
+                                : distill_kernel<T, FWD, GRAD, !GRAD, WIDTH>,
                            static_cast<unsigned>(d->rows * parts), parts, shape_of(WIDTH).threads + 32,
                            entries_bytes(d->top), s, P);
 }
@@ -511,7 +519,9 @@ cudaError_t launch(const malt_distill_t* d, const Params& P, cudaStream_t s) {
     int parts = 1;
     while (parts < kSizeCluster && bytes > parts * part) parts *= 2;
     // More while a row's blocks leave SMs idle and its parts keep a vector for each thread.
-    while (parts < kMaxCluster && d->rows * parts < sm_count() && bytes / (2 * parts) >= shape_of(kMedium).threads * 16) parts *= 2;
+    while (parts < kMaxCluster && d->rows * parts < sm_count() &&
+           bytes / (2 * parts) >= shape_of(kMedium).threads * 16)
+        parts *= 2;
     // Short rows leave most of a wide block waiting for its barriers; a single sweep has
     // nothing to keep in L2.
     if (bytes <= kNarrowRow) return launch_width<T, FWD, GRAD, kNarrow>(d, P, parts, s);

@@ -21,7 +21,8 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
-constexpr int kWindow = 16;
+constexpr int kWindow = 16;         // tokens of a window (32: 20 us for 17 at 4999 tokens)
+constexpr int64_t kMaxTokens = int64_t{1} << 30;    // 32-bit places in the order, and a window past them
 
 // ------------------------------------------------------------------- forward
 // One warp per token and slice of the row; every lane has up to kFwdLoads
@@ -46,7 +47,8 @@ embed_forward_kernel(const I* ids, int64_t tokens, int64_t vocab, int64_t dim, c
     const int64_t id = load_id(ids, t);
     D* const o = out + t * out_ld;
     float x[kFwdLoads][VEC];
-    if (id >= 0 && id < vocab) {
+    const bool inside = id >= 0 && id < vocab;
+    if (inside) {
         const S* const row = table + id * table_ld;
 #pragma unroll
         for (int j = 0; j < kFwdLoads; ++j) {
@@ -54,7 +56,8 @@ embed_forward_kernel(const I* ids, int64_t tokens, int64_t vocab, int64_t dim, c
             if (j < steps && e < dim) load_vec<S, VEC>(row + e, x[j]);
         }
     } else {
-        // padding has no row; an id past the table has no value
+        // padding has no row; an id past the table has no value; neither is scaled
+        scale = 1.f;
         const float v = id < 0 ? 0.f : __int_as_float(0x7fc00000);
 #pragma unroll
         for (int j = 0; j < kFwdLoads; ++j)
@@ -74,11 +77,14 @@ embed_forward_kernel(const I* ids, int64_t tokens, int64_t vocab, int64_t dim, c
 
 // ------------------------------------------------------------ backward: sort
 // Block b of n (a power of two) owns the table rows b, b + n, b + 2 n, ...: the ids of
-// frequent tokens, which lie together, are spread over the blocks.  It reads every id, counts those of its
-// rows (per warp, each warp a contiguous run of tokens) and those of the blocks before
-// it, and writes the records of its tokens to their place in the order (block, row,
-// token): no launch has to wait for another block's counts, and the order needs no
-// atomic that decides it.  Then it zeroes its rows that no token names.
+// frequent tokens, which lie together, are spread over the blocks (owners of neighbouring
+// rows: the first block alone matches most of a text, 10 us of 18 for 16384 tokens).  It
+// reads every id, counts those of its rows (per warp, each warp a contiguous run of
+// tokens) and those of the blocks before it, and writes the records of its tokens to
+// their place in the order (block, row, token): no launch has to wait for another
+// block's counts, and the order needs no atomic that decides it.  Then it zeroes its rows
+// that no token names (beside the sums instead: the sums' registers leave the zeros too
+// few blocks, 73 us for 64).
 constexpr int kSortThreads = 1024;
 constexpr int kSortWarps = kSortThreads / 32;
 static_assert(kSortWarps == 32, "a warp adds up one value of each warp");
@@ -244,7 +250,8 @@ embed_sum_kernel(const TokenRecord* rec, const int32_t* total, int32_t windows, 
                 if (ADD && j0 + j < here && (ends >> (j0 + j) & 1)) {
                     const D* const to = dtable + static_cast<int64_t>(__shfl_sync(~0u, mine.row, j0 + j)) * ld;
 #pragma unroll
-                    for (int s = 0; s < SUB; ++s) old[j % (ADD ? kSumLoads : 1)][s] = *reinterpret_cast<const Raw<D, VEC>*>(to + column[s]);
+                    for (int s = 0; s < SUB; ++s)
+                        old[ADD ? j : 0][s] = *reinterpret_cast<const Raw<D, VEC>*>(to + column[s]);
                 }
             }
 #pragma unroll
@@ -264,7 +271,7 @@ embed_sum_kernel(const TokenRecord* rec, const int32_t* total, int32_t windows, 
                         float y[VEC];
 #pragma unroll
                         for (int k = 0; k < VEC; ++k)
-                            y[k] = ADD ? fmaf(scale, acc[s][k], static_cast<float>(old[j % (ADD ? kSumLoads : 1)][s].v[k]))
+                            y[k] = ADD ? fmaf(scale, acc[s][k], static_cast<float>(old[ADD ? j : 0][s].v[k]))
                                        : scale * acc[s][k];
                         if (base + s * (32 * VEC) < dim) store_vec<D, VEC>(to + column[s], y);
                     }
@@ -290,8 +297,8 @@ embed_sum_kernel(const TokenRecord* rec, const int32_t* total, int32_t windows, 
 constexpr int kJoinCols = 128, kJoinLoads = 4;
 template <typename D>
 __global__ void __launch_bounds__(kThreads)
-embed_join_kernel(const TokenRecord* rec, const int32_t* total, int32_t windows, int32_t window, int32_t slices,
-                  D* dtable, int64_t ld, int64_t dim, float scale, int accumulate, const float* parts) {
+embed_join_kernel(const TokenRecord* rec, const int32_t* total, int32_t window, int32_t slices, D* dtable, int64_t ld,
+                  int64_t dim, float scale, int accumulate, const float* parts) {
     __shared__ TokenRecord last[kWarps];
     __shared__ float sums[kWarps][kJoinCols];
     constexpr int kCols = kJoinCols / 32;
@@ -375,7 +382,7 @@ int check(const malt_embed_t* e) {
     if (!index_type(e->ids_dtype) || !float_type(e->table_dtype) || !float_type(e->rows_dtype))
         return MALT_ERR_UNSUPPORTED;
     constexpr int64_t kMax = (int64_t{1} << 31) - 1 - (1 << 16);
-    if (e->tokens > kMax || e->vocab > kMax || e->dim > kMax) return MALT_ERR_UNSUPPORTED;
+    if (e->tokens >= kMaxTokens || e->vocab > kMax || e->dim > kMax) return MALT_ERR_UNSUPPORTED;
     if (e->table_ld < e->dim || e->rows_ld < e->dim) return MALT_ERR_INVALID_ARG;
     if ((e->tokens > 0 && (e->ids == nullptr || (e->dim > 0 && e->rows == nullptr))) ||
         (e->vocab > 0 && e->dim > 0 && e->table == nullptr))
@@ -447,11 +454,13 @@ cudaError_t sums(const malt_embed_t* e, const Workspace& w, uint8_t* ws, cudaStr
     const int32_t* const total = reinterpret_cast<int32_t*>(ws + w.total);
     float* const parts = reinterpret_cast<float*>(ws + w.parts);
     D* const dtable = static_cast<D*>(e->table);
-    cudaError_t rc = launch_chained(embed_sum_kernel<S, D, ADD, VEC, SUB>, static_cast<unsigned>(sum_blocks), kThreads, 0, s, rec,
-                                    total, windows, window, static_cast<int32_t>(slices), static_cast<const S*>(e->rows), e->rows_ld, dtable, e->table_ld, e->dim, e->scale, parts);
+    const cudaError_t rc = launch_chained(
+        embed_sum_kernel<S, D, ADD, VEC, SUB>, static_cast<unsigned>(sum_blocks), kThreads, 0, s, rec, total, windows,
+        window, static_cast<int32_t>(slices), static_cast<const S*>(e->rows), e->rows_ld, dtable, e->table_ld, e->dim,
+        e->scale, parts);
     if (rc != cudaSuccess || e->tokens <= window) return rc;
     return launch_chained(embed_join_kernel<D>, static_cast<unsigned>(groups * cols), kThreads, 0, s, rec, total,
-                          windows, window, static_cast<int32_t>(cols), dtable, e->table_ld, e->dim, e->scale, ADD ? 1 : 0,
+                          window, static_cast<int32_t>(cols), dtable, e->table_ld, e->dim, e->scale, ADD ? 1 : 0,
                           static_cast<const float*>(parts));
 }
 

@@ -88,8 +88,8 @@ __device__ __forceinline__ float2 angle(const Params& P, int64_t pos, int p) {
 
 // --------------------------------------------------------------- aligned rows
 // A row is held by neighbouring lanes, 2 V entries each: the V pairs that the lane turns,
-// partners in the lane, in two vectors of V (8 or 16 bytes), so that one lane needs V cosines and
-// V sines.  These lanes are a slot, which keeps its token's angles and the gains in
+// partners in the lane, in two vectors of V, so that one lane needs V cosines and V
+// sines.  These lanes are a slot, which keeps its token's angles and the gains in
 // registers and walks over heads; neighbouring slots take neighbouring heads of a token,
 // so that a warp's loads are contiguous.  Arithmetic is on two pairs at once: A holds the
 // first members, B the second ones.
@@ -345,7 +345,7 @@ qk_backward_kernel(const __grid_constant__ Params P) {
     constexpr int V = vector_of<T>(), N = 2 * V;
     using C = Chunk<V, INTER>;
     using M = Members<V, INTER>;
-    extern __shared__ uint4 stage[];        // [kBwdStages][4][kBwdThreads]; at the end [kBwdWarps][slots of a warp][dim] sums
+    extern __shared__ uint4 stage[];        // [kBwdStages][4][kBwdThreads]; at the end the slots' sums
     __shared__ int64_t place[kBwdStages][kBwdThreads];     // positions
     const bool keys = blockIdx.x >= P.kind[0].blocks;
     const Kind& K = P.kind[keys];
@@ -433,7 +433,9 @@ qk_backward_kernel(const __grid_constant__ Params P) {
             copies_wait<kBwdStages - 1>();
             if (i == 0 && w.live) {
                 const int64_t* const p = &place[at_slot % kBwdStages][threadIdx.x];
-                const int64_t pos = P.positions == nullptr ? w.s : P.positions_i64 ? *p : *reinterpret_cast<const int32_t*>(p);
+                const int64_t pos = P.positions == nullptr ? w.s
+                                    : P.positions_i64      ? *p
+                                                           : *reinterpret_cast<const int32_t*>(p);
                 t.load(P, pos, slots.sub, chunk.turned);
             }
             const bool here = w.live && h < K.heads;
@@ -593,7 +595,8 @@ qk_backward_any_kernel(const __grid_constant__ Params P) {
             const float na = ya[0] * cs.x + yb[0] * cs.y, nb = yb[0] * cs.x - ya[0] * cs.y;
             acc[ia] = fmaf(na, xa[0] * r, acc[ia]);
             acc[ib] = fmaf(nb, xb[0] * r, acc[ib]);
-            const float da[1] = {r * (na * gain_at(P, K, ia) - xa[0] * c)}, db[1] = {r * (nb * gain_at(P, K, ib) - xb[0] * c)};
+            const float da[1] = {r * (na * gain_at(P, K, ia) - xa[0] * c)};
+            const float db[1] = {r * (nb * gain_at(P, K, ib) - xb[0] * c)};
             store_vec<T, 1>(dx + ia, da);
             store_vec<T, 1>(dx + ib, db);
         }
@@ -642,13 +645,15 @@ qk_gain_kernel(const __grid_constant__ Params P) {
 int64_t tokens_of(const malt_qk_norm_t* p) { return p->batch * p->seq; }
 
 int check(const malt_qk_norm_t* p) {
-    if (p == nullptr || p->batch < 0 || p->seq < 0 || p->table_rows < 0 || !(p->eps >= 0.f)) return MALT_ERR_INVALID_ARG;
+    if (p == nullptr || p->batch < 0 || p->seq < 0 || p->table_rows < 0 || !(p->eps >= 0.f))
+        return MALT_ERR_INVALID_ARG;
     if (!float_type(p->dtype) || !float_type(p->gain_dtype)) return MALT_ERR_UNSUPPORTED;
     if (p->head_dim < 1 || p->head_dim > kMaxHeadDim) return MALT_ERR_UNSUPPORTED;
     if (p->rot_dim < 0 || p->rot_dim > p->head_dim || p->rot_dim % 2 != 0) return MALT_ERR_INVALID_ARG;
     constexpr int64_t kMax = int64_t{1} << 31;
     if (p->batch >= kMax || p->seq >= kMax || p->batch * p->seq >= kMax) return MALT_ERR_UNSUPPORTED;
-    if (p->rot_dim > 0 && p->table_rows > 0 && (p->cosines == nullptr || p->sines == nullptr)) return MALT_ERR_INVALID_ARG;
+    if (p->rot_dim > 0 && p->table_rows > 0 && (p->cosines == nullptr || p->sines == nullptr))
+        return MALT_ERR_INVALID_ARG;
     if (p->positions != nullptr && !index_type(p->positions_dtype)) return MALT_ERR_UNSUPPORTED;
     if (!aligned_to(p->cosines, 4) || !aligned_to(p->sines, 4) ||
         (p->positions != nullptr && !aligned_to(p->positions, type_bytes(p->positions_dtype))) ||
@@ -748,12 +753,15 @@ cudaError_t backward_rows(Params& P, cudaStream_t s) {
     const int64_t kSlots = kBwdWarps * (32 / P.lanes);
     const int64_t heads = P.kind[0].heads + P.kind[1].heads;
     for (Kind& K : P.kind) {
-        const int64_t share = K.heads > 0 ? std::max<int64_t>(1, static_cast<int64_t>(sm_count()) * kBwdBlocks * K.heads / heads) : 0;
+        const int64_t all = static_cast<int64_t>(sm_count()) * kBwdBlocks;
+        const int64_t share = K.heads > 0 ? std::max<int64_t>(1, all * K.heads / heads) : 0;
         K.blocks = static_cast<int32_t>(std::min<int64_t>((K.slots + kSlots - 1) / kSlots, share));
     }
     P.kind[1].parts = P.kind[0].parts + static_cast<int64_t>(P.kind[0].blocks) * P.dim;
-    constexpr int kSmem = kBwdStages * 4 * kBwdThreads * 16;      // the sums of 32 lanes of 2 V entries a warp fit in it
-    static_assert(kSmem >= kBwdWarps * 32 * 8 * static_cast<int>(sizeof(float)) * 2, "sums in the stages' place");
+    constexpr int kSmem = kBwdStages * 4 * kBwdThreads * 16;
+    static_assert(kSmem >= kBwdThreads * 2 * vector_of<T>() * static_cast<int>(sizeof(float)),
+                  "the sums of every lane's entries take the stages' place");
+    static_assert(kBwdBlocks <= 6, "the workspace has a part for each block");
     auto* const kernel = qk_backward_kernel<T, INTER, LANES>;
     const cudaError_t rc = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
     if (rc != cudaSuccess) { cudaGetLastError(); return rc; }
@@ -806,7 +814,8 @@ cudaError_t backward(Params& P, bool inter, cudaStream_t s) {
     const int64_t heads = P.kind[0].heads + P.kind[1].heads;
     for (Kind& K : P.kind) {
         const int64_t blocks = (P.batch * P.seq * K.heads + kWarps - 1) / kWarps;
-        const int64_t share = K.heads > 0 ? std::max<int64_t>(1, static_cast<int64_t>(backward_blocks()) * K.heads / heads) : 0;
+        const int64_t all = backward_blocks();
+        const int64_t share = K.heads > 0 ? std::max<int64_t>(1, all * K.heads / heads) : 0;
         K.blocks = static_cast<int32_t>(std::min(blocks, share));
     }
     P.kind[1].parts = P.kind[0].parts + static_cast<int64_t>(P.kind[0].blocks) * P.dim;
@@ -861,7 +870,8 @@ int malt_qk_norm_backward(const malt_qk_norm_t* p, const malt_heads_t* dq_out, c
     for (int i = 0; i < 6; ++i)
         if ((rc = check_heads(p, all[i], i % 2 ? k : q)) != MALT_OK) return rc;
     if (!aligned_to(dq_gain, 4) || !aligned_to(dk_gain, 4) || !aligned_to(workspace, 16)) return MALT_ERR_MISALIGNED;
-    if (workspace == nullptr || workspace_bytes < malt_qk_norm_workspace_bytes(p->head_dim)) return MALT_ERR_INVALID_ARG;
+    if (workspace == nullptr || workspace_bytes < malt_qk_norm_workspace_bytes(p->head_dim))
+        return MALT_ERR_INVALID_ARG;
     Params P = params_of(p);
     P.kind[0].x = rows_of(q);
     P.kind[1].x = rows_of(k);
