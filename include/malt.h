@@ -463,7 +463,7 @@ void malt_adamw_destroy_state(malt_adamw_state_t* st);
  * row is zero and it adds nothing.  An id >= vocab is an error of the caller
  * that costs no memory safety: its output row is NaN, and it adds nothing.
  * Sums are fp32 in the order of the tokens, in windows of a length that
- * depends on `tokens` only.  tokens < 2^30; vocab, dim < 2^31 - 2^16. */
+ * depends on `tokens` only.  tokens < 2^30, vocab < 2^31 - 2^16, dim <= 2^24. */
 typedef struct {
     const void* ids;            /* tokens ids, MALT_I32 or MALT_I64          */
     int32_t     ids_dtype;

@@ -6,10 +6,10 @@
 // their own order, long runs in windows of a fixed length.
 //
 // Both are bound by HBM, and every row of the gradient is written once.  40960 tokens
-// of 1280 from bf16 rows to fp32: 42 us, 5.7 TB/s.  The gradient of 16384 of them to a
-// table of 50304 rows, bf16 to fp32: 64 us, 4.7 TB/s (the order and the zero rows 39,
-// of which the zeros alone take 25, the sums 18, the long rows 7); in place of 4999 x 501
-// fp32: 17 us, bound by the three launches' latencies.
+// of 1280 from bf16 rows to fp32: 42 us, 5.7 TB/s (a copy of as many bytes 6.0).  The
+// gradient of 16384 of them to a table of 50304 rows, bf16 to fp32: 60 us, 5.0 TB/s (the
+// order and the zero rows 39, of which the zeros alone take 25; the sums 20); added in
+// place for 4999 x 501 fp32: 13.6 us, bound by the two launches' latencies.
 #include <algorithm>
 
 #include <nvtx3/nvToolsExt.h>
@@ -22,6 +22,8 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
 constexpr int kWindow = 16;         // tokens of a window (32: 20 us for 17 at 4999 tokens)
+constexpr int kLeastSlice = 64;     // columns that a warp sums, at least
+constexpr int64_t kMaxDim = int64_t{1} << 24;       // 32-bit counts of windows and slices
 constexpr int64_t kMaxTokens = int64_t{1} << 30;    // 32-bit places in the order, and a window past them
 
 // ------------------------------------------------------------------- forward
@@ -83,8 +85,8 @@ embed_forward_kernel(const I* ids, int64_t tokens, int64_t vocab, int64_t dim, c
 // tokens) and those of the blocks before it, and writes the records of its tokens to
 // their place in the order (block, row, token): no launch has to wait for another
 // block's counts, and the order needs no atomic that decides it.  Then it zeroes its rows
-// that no token names (beside the sums instead: the sums' registers leave the zeros too
-// few blocks, 73 us for 64).
+// that no token names (beside the sums, by warps or blocks of their own, the zeros' stores
+// hold up the sums' loads: 62 to 73 us for 58).
 constexpr int kSortThreads = 1024;
 constexpr int kSortWarps = kSortThreads / 32;
 static_assert(kSortWarps == 32, "a warp adds up one value of each warp");
@@ -99,7 +101,7 @@ struct __align__(16) TokenRecord {
 template <typename I, typename D, int VEC>
 __global__ void __launch_bounds__(kSortThreads)
 embed_sort_kernel(const I* ids, int32_t tokens, int32_t vocab, int shift, int32_t owned, TokenRecord* rec,
-                  int32_t* total, D* dtable, int64_t ld, int64_t dim, int fill) {
+                  int32_t* total, uint32_t* arrived, int32_t counters, D* dtable, int64_t ld, int64_t dim, int fill) {
     extern __shared__ uint32_t smem[];
     uint32_t* const place = smem;                               // [kSortWarps][owned]
     int32_t* const row_begin = reinterpret_cast<int32_t*>(smem + kSortWarps * owned);
@@ -112,6 +114,7 @@ embed_sort_kernel(const I* ids, int32_t tokens, int32_t vocab, int shift, int32_
     for (int i = threadIdx.x; i < kSortWarps * owned; i += kSortThreads) place[i] = 0;
     __syncthreads();
     chain_wait();
+    for (int64_t i = blockIdx.x * kSortThreads + threadIdx.x; i < counters; i += gridDim.x * kSortThreads) arrived[i] = 0;
 
     const int32_t per = (tokens / kSortWarps / 32 + 1) * 32;
     const int32_t lo = static_cast<int32_t>(min(static_cast<int64_t>(warp) * per, static_cast<int64_t>(tokens)));
@@ -206,24 +209,57 @@ embed_sort_kernel(const I* ids, int32_t tokens, int32_t vocab, int shift, int32_
 // ------------------------------------------------------------- backward: sums
 // A warp takes a window of the sorted tokens and a slice of the row.  A row of at
 // most `window` tokens is summed by the window that it begins in, whole; a longer
-// one in parts, a part per window, which the join launch adds up.
+// one in parts, a part per window, which the last of its windows to arrive adds up in
+// their order.
+// The parts of windows w0 .. w1 of a row, a slice of it, in the windows' order.
+template <typename D, bool ADD, int VEC, int SUB>
+__device__ __forceinline__ void join_parts(const float* parts, int32_t w0, int32_t w1, int64_t base, int64_t dim, D* row,
+                                           float scale) {
+    constexpr int kLoads = 8;
+#pragma unroll
+    for (int s = 0; s < SUB; ++s) {
+        const int64_t e = base + s * (32 * VEC);
+        if (e >= dim) continue;
+        float acc[VEC] = {};
+        for (int32_t k0 = w0; k0 <= w1; k0 += kLoads) {
+            float x[kLoads][VEC];
+#pragma unroll
+            for (int u = 0; u < kLoads; ++u) {
+                const int32_t k = min(k0 + u, w1);
+                load_l2<VEC>(parts + (static_cast<int64_t>(k) * 2 + (k == w0)) * dim + e, x[u]);
+            }
+#pragma unroll
+            for (int u = 0; u < kLoads; ++u)
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) acc[i] += k0 + u <= w1 ? x[u][i] : 0.f;
+        }
+        float y[VEC] = {};
+        if (ADD) load_vec<D, VEC>(row + e, y);
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) y[i] = ADD ? fmaf(scale, acc[i], y[i]) : scale * acc[i];
+        store_vec<D, VEC>(row + e, y);
+    }
+}
 
-// ADD: to what the table holds, whose rows are loaded with the tokens that end them.
+constexpr int kSumLoads = 8;        // tokens in flight
+
+// ADD: to what the table holds, whose rows are loaded with the tokens that end them (that
+// takes the registers of two blocks of an SM; without, four: 60 us for 65 at two).
 template <typename S, typename D, bool ADD, int VEC, int SUB>
-__global__ void __launch_bounds__(kThreads)
-embed_sum_kernel(const TokenRecord* rec, const int32_t* total, int32_t windows, int32_t window, int32_t slices,
-                 const S* dout, int64_t dout_ld, D* dtable, int64_t ld, int64_t dim, float scale, float* parts) {
-    constexpr int kSumLoads = ADD ? 8 : 16;      // tokens in flight
+__global__ void __launch_bounds__(kThreads, ADD ? 2 : 4)
+embed_sum_kernel(const TokenRecord* rec, const int32_t* total, int32_t windows, int32_t window, int32_t slices, const S* dout, int64_t dout_ld, D* dtable, int64_t ld, int64_t dim, float scale, float* parts,
+                 uint32_t* arrived) {
     chain_wait();
     const int32_t n = *after_wait(total);
     const int lane = threadIdx.x & 31;
+    rec = after_wait(rec);
     const int64_t item = static_cast<int64_t>(blockIdx.x) * kWarps + (threadIdx.x >> 5);
     const int32_t w = static_cast<int32_t>(item / slices);
     if (w >= windows) return;
-    const int64_t base = (item - static_cast<int64_t>(w) * slices) * (32 * VEC * SUB) + lane * VEC;
+    const int32_t slice = static_cast<int32_t>(item - static_cast<int64_t>(w) * slices);
+    const int64_t base = static_cast<int64_t>(slice) * (32 * VEC * SUB) + lane * VEC;
     const int32_t a = w * window, b = min(n, a + window);
     if (a >= n) return;
-    rec = after_wait(rec);
     // From the first token that is no tail of a row of the window before, to the end of
     // the last row that this window sums whole.
     const TokenRecord head = rec[a], tail = rec[b - 1];
@@ -281,75 +317,22 @@ embed_sum_kernel(const TokenRecord* rec, const int32_t* total, int32_t windows, 
 #pragma unroll
                     for (int s = 0; s < SUB; ++s)
                         if (base + s * (32 * VEC) < dim) store_vec<float, VEC>(part + column[s], acc[s]);
+                    // The last window of the row to arrive adds up the parts.
+                    const int32_t w0 = begin / window, w1 = (end - 1) / window;
+                    uint32_t before = 0;
+                    __threadfence();
+                    __syncwarp();
+                    if (lane == 0) before = atomicAdd(arrived + static_cast<int64_t>(w0) * slices + slice, 1u);
+                    if (__shfl_sync(~0u, before, 0) == static_cast<uint32_t>(w1 - w0)) {
+                        __threadfence();
+                        join_parts<D, ADD, VEC, SUB>(parts, w0, w1, base, dim, dtable + static_cast<int64_t>(row) * ld, scale);
+                    }
                 }
 #pragma unroll
                 for (int s = 0; s < SUB; ++s)
 #pragma unroll
                     for (int k = 0; k < VEC; ++k) acc[s][k] = 0.f;
             }
-        }
-    }
-}
-
-// The rows of more than `window` tokens: a block looks at kWarps windows, and takes
-// kJoinCols columns of each such row that begins last in one of them, each warp every
-// kWarps-th of the row's parts.
-constexpr int kJoinCols = 128, kJoinLoads = 4;
-template <typename D>
-__global__ void __launch_bounds__(kThreads)
-embed_join_kernel(const TokenRecord* rec, const int32_t* total, int32_t window, int32_t slices, D* dtable, int64_t ld,
-                  int64_t dim, float scale, int accumulate, const float* parts) {
-    __shared__ TokenRecord last[kWarps];
-    __shared__ float sums[kWarps][kJoinCols];
-    constexpr int kCols = kJoinCols / 32;
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int32_t group = blockIdx.x / slices;
-    const int64_t base = static_cast<int64_t>(blockIdx.x - group * slices) * kJoinCols;
-    chain_wait();
-    const int32_t n = *after_wait(total);
-    if (threadIdx.x < kWarps) {
-        const int64_t a = (static_cast<int64_t>(group) * kWarps + threadIdx.x) * window;
-        TokenRecord r = {0, 0, 0, 0};
-        if (a < n) r = after_wait(rec)[min(static_cast<int64_t>(n), a + window) - 1];
-        if (r.begin < a) r.end = r.begin;       // another window's
-        last[threadIdx.x] = r;
-    }
-    __syncthreads();
-    parts = after_wait(parts);
-    for (int i = 0; i < kWarps; ++i) {
-        const TokenRecord r = last[i];
-        if (r.end - r.begin <= window) continue;
-        const int32_t w = group * kWarps + i, w_end = (r.end - 1) / window;
-        float acc[kCols] = {};
-        for (int32_t k0 = w + warp; k0 <= w_end; k0 += kWarps * kJoinLoads) {
-            float x[kJoinLoads][kCols];
-#pragma unroll
-            for (int u = 0; u < kJoinLoads; ++u) {
-                const int32_t k = k0 + u * kWarps;
-#pragma unroll
-                for (int c = 0; c < kCols; ++c) {
-                    const int64_t e = base + c * 32 + lane;
-                    x[u][c] = k <= w_end && e < dim ? parts[(static_cast<int64_t>(k) * 2 + (k == w)) * dim + e] : 0.f;
-                }
-            }
-#pragma unroll
-            for (int u = 0; u < kJoinLoads; ++u)
-#pragma unroll
-                for (int c = 0; c < kCols; ++c) acc[c] += x[u][c];
-        }
-        __syncthreads();
-#pragma unroll
-        for (int c = 0; c < kCols; ++c) sums[warp][c * 32 + lane] = acc[c];
-        __syncthreads();
-        const int64_t e = base + threadIdx.x;
-        if (threadIdx.x < kJoinCols && e < dim) {
-            float y[1] = {0.f}, old[1] = {0.f};
-#pragma unroll
-            for (int k = 0; k < kWarps; ++k) y[0] += sums[k][threadIdx.x];
-            D* const to = dtable + static_cast<int64_t>(r.row) * ld + e;
-            if (accumulate) load_vec<D, 1>(to, old);
-            y[0] = fmaf(scale, y[0], old[0]);
-            store_vec<D, 1>(to, y);
         }
     }
 }
@@ -364,14 +347,17 @@ int32_t window_length(int64_t tokens) {
 }
 
 struct Workspace {
-    size_t rec, total, parts, bytes;
+    size_t rec, total, arrived, parts, bytes;
+    int32_t counters;       // a counter for each window and slice of a row, where rows may be long
 };
 Workspace workspace_of(int64_t tokens, int64_t dim) {
     const int64_t window = window_length(tokens), windows = (tokens + window - 1) / window;
     Workspace w;
     w.rec = 0;
     w.total = static_cast<size_t>(tokens) * sizeof(TokenRecord);
-    w.parts = w.total + 256;
+    w.arrived = w.total + 256;
+    w.counters = tokens > window ? static_cast<int32_t>(windows * ((dim + kLeastSlice - 1) / kLeastSlice)) : 0;
+    w.parts = w.arrived + (static_cast<size_t>(w.counters) * sizeof(uint32_t) + 255) / 256 * 256;
     w.bytes = w.parts + (tokens > window ? static_cast<size_t>(windows) * 2 * dim * sizeof(float) : 0);
     return w;
 }
@@ -382,7 +368,7 @@ int check(const malt_embed_t* e) {
     if (!index_type(e->ids_dtype) || !float_type(e->table_dtype) || !float_type(e->rows_dtype))
         return MALT_ERR_UNSUPPORTED;
     constexpr int64_t kMax = (int64_t{1} << 31) - 1 - (1 << 16);
-    if (e->tokens >= kMaxTokens || e->vocab > kMax || e->dim > kMax) return MALT_ERR_UNSUPPORTED;
+    if (e->tokens >= kMaxTokens || e->vocab > kMax || e->dim > kMaxDim) return MALT_ERR_UNSUPPORTED;
     if (e->table_ld < e->dim || e->rows_ld < e->dim) return MALT_ERR_INVALID_ARG;
     if ((e->tokens > 0 && (e->ids == nullptr || (e->dim > 0 && e->rows == nullptr))) ||
         (e->vocab > 0 && e->dim > 0 && e->table == nullptr))
@@ -415,8 +401,8 @@ cudaError_t forward(const malt_embed_t* e, cudaStream_t s) {
 
 template <typename I, typename D, int VEC>
 cudaError_t sort(const malt_embed_t* e, const Workspace& w, uint8_t* ws, bool add, cudaStream_t s) {
-    // Of the powers of two the largest that the SMs hold at once, more for a table of more
-    // rows than these can own.
+    // Blocks, as a power of two: the largest that the SMs hold at once, more for a table of
+    // more rows than these can own.
     int shift = 0;
     while ((2 << shift) <= sm_count()) ++shift;
     while ((int64_t{kMaxOwned} << shift) < e->vocab) ++shift;
@@ -432,7 +418,8 @@ cudaError_t sort(const malt_embed_t* e, const Workspace& w, uint8_t* ws, bool ad
     return launch_chained(kernel, static_cast<unsigned>(blocks), kSortThreads, smem, s, static_cast<const I*>(e->ids),
                           static_cast<int32_t>(e->tokens), static_cast<int32_t>(e->vocab), shift, owned,
                           reinterpret_cast<TokenRecord*>(ws + w.rec), reinterpret_cast<int32_t*>(ws + w.total),
-                          static_cast<D*>(e->table), e->table_ld, e->dim, add ? 0 : 1);
+                          reinterpret_cast<uint32_t*>(ws + w.arrived), w.counters, static_cast<D*>(e->table),
+                          e->table_ld, e->dim, add ? 0 : 1);
 }
 
 template <typename I, typename D>
@@ -447,21 +434,14 @@ cudaError_t sums(const malt_embed_t* e, const Workspace& w, uint8_t* ws, cudaStr
     const int32_t window = window_length(e->tokens);
     const int32_t windows = static_cast<int32_t>((e->tokens + window - 1) / window);
     const int64_t slices = (e->dim + 32 * VEC * SUB - 1) / (32 * VEC * SUB);
-    const int64_t sum_blocks = (windows * slices + kWarps - 1) / kWarps;
-    const int64_t cols = (e->dim + kJoinCols - 1) / kJoinCols, groups = (windows + kWarps - 1) / kWarps;
-    if (sum_blocks >= (int64_t{1} << 31) || groups * cols >= (int64_t{1} << 31)) return cudaErrorInvalidValue;
-    const TokenRecord* const rec = reinterpret_cast<TokenRecord*>(ws + w.rec);
-    const int32_t* const total = reinterpret_cast<int32_t*>(ws + w.total);
-    float* const parts = reinterpret_cast<float*>(ws + w.parts);
-    D* const dtable = static_cast<D*>(e->table);
-    const cudaError_t rc = launch_chained(
-        embed_sum_kernel<S, D, ADD, VEC, SUB>, static_cast<unsigned>(sum_blocks), kThreads, 0, s, rec, total, windows,
-        window, static_cast<int32_t>(slices), static_cast<const S*>(e->rows), e->rows_ld, dtable, e->table_ld, e->dim,
-        e->scale, parts);
-    if (rc != cudaSuccess || e->tokens <= window) return rc;
-    return launch_chained(embed_join_kernel<D>, static_cast<unsigned>(groups * cols), kThreads, 0, s, rec, total,
-                          window, static_cast<int32_t>(cols), dtable, e->table_ld, e->dim, e->scale, ADD ? 1 : 0,
-                          static_cast<const float*>(parts));
+    static_assert(32 * VEC * SUB >= kLeastSlice, "counters for narrower slices");
+    const int64_t blocks = (windows * slices + kWarps - 1) / kWarps;
+    if (blocks >= (int64_t{1} << 31)) return cudaErrorInvalidValue;
+    return launch_chained(embed_sum_kernel<S, D, ADD, VEC, SUB>, static_cast<unsigned>(blocks), kThreads, 0, s,
+                          reinterpret_cast<const TokenRecord*>(ws + w.rec), reinterpret_cast<const int32_t*>(ws + w.total),
+                          windows, window, static_cast<int32_t>(slices), static_cast<const S*>(e->rows), e->rows_ld,
+                          static_cast<D*>(e->table), e->table_ld, e->dim, e->scale,
+                          reinterpret_cast<float*>(ws + w.parts), reinterpret_cast<uint32_t*>(ws + w.arrived));
 }
 
 template <typename I>

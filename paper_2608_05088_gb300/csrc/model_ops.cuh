@@ -106,6 +106,18 @@ __device__ __forceinline__ void store_vec(T* p, const float (&x)[VEC]) {
     }
 }
 
+// VEC (1 or 4) floats that another SM may have written in this launch: from L2.
+template <int VEC>
+__device__ __forceinline__ void load_l2(const float* p, float (&x)[VEC]) {
+    static_assert(VEC == 1 || VEC == 4);
+    if constexpr (VEC == 1) {
+        x[0] = __ldcg(p);
+    } else {
+        const float4 a = __ldcg(reinterpret_cast<const float4*>(p));
+        x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w;
+    }
+}
+
 // ---------------------------------------------------------------- reductions
 __device__ __forceinline__ float warp_sum(float v) {
 #pragma unroll
