@@ -21,8 +21,9 @@
 //
 // An exponent s c - m c is one fused multiply-add of the rounded product m c, whose
 // rounding is the same for every entry and is taken out of the sum again at its end.
-// Where that product leaves fp32's range (a row of the type's lowest values is a
-// uniform one) the difference is taken first.
+// Where that product is so large that its rounding is no small exponent (a cold
+// temperature, or a row of the type's lowest values, which is a uniform one) the
+// difference is taken first.
 #include <algorithm>
 #include <cooperative_groups.h>
 
@@ -125,8 +126,9 @@ __device__ __forceinline__ float largest(const uint4 (&u)[N]) {
     }
 }
 
-// The products that exponents are taken from stay far inside fp32's range.
-__device__ __forceinline__ bool in_range(float product) { return fabsf(product) < 1e30f; }
+// A product m c whose rounding (half an ulp, 2^-5 here at most) is a small exponent that
+// the sum can be corrected by; past it, and past fp32's range, differences come first.
+__device__ __forceinline__ bool in_range(float product) { return fabsf(product) < 0x1p20f; }
 
 // Running maximum and sum of a thread, the sum in two halves relative to `ref`, the
 // rounded product m c.
@@ -320,8 +322,8 @@ struct Gradient {
 // The listed entries of [begin, end), written again with their target by `threads`
 // threads.  An entry listed twice is written twice with the same sum.
 template <typename T>
-__device__ __forceinline__ void store_targets(const Params& P, const Gradient& g, const Top& top, int begin, int end, T* dx,
-                                              int first, int threads) {
+__device__ __forceinline__ void store_targets(const Params& P, const Gradient& g, const Top& top, int begin, int end,
+                                              T* dx, int first, int threads) {
     for (int j = first; j < P.top; j += threads) {
         const int32_t id = top.id[j];
         if (id < begin || id >= end) continue;

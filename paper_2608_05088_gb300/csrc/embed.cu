@@ -114,7 +114,8 @@ embed_sort_kernel(const I* ids, int32_t tokens, int32_t vocab, int shift, int32_
     for (int i = threadIdx.x; i < kSortWarps * owned; i += kSortThreads) place[i] = 0;
     __syncthreads();
     chain_wait();
-    for (int64_t i = blockIdx.x * kSortThreads + threadIdx.x; i < counters; i += gridDim.x * kSortThreads) arrived[i] = 0;
+    for (int64_t i = blockIdx.x * kSortThreads + threadIdx.x; i < counters; i += gridDim.x * kSortThreads)
+        arrived[i] = 0;
 
     const int32_t per = (tokens / kSortWarps / 32 + 1) * 32;
     const int32_t lo = static_cast<int32_t>(min(static_cast<int64_t>(warp) * per, static_cast<int64_t>(tokens)));
@@ -247,7 +248,8 @@ constexpr int kSumLoads = 8;        // tokens in flight
 // takes the registers of two blocks of an SM; without, four: 60 us for 65 at two).
 template <typename S, typename D, bool ADD, int VEC, int SUB>
 __global__ void __launch_bounds__(kThreads, ADD ? 2 : 4)
-embed_sum_kernel(const TokenRecord* rec, const int32_t* total, int32_t windows, int32_t window, int32_t slices, const S* dout, int64_t dout_ld, D* dtable, int64_t ld, int64_t dim, float scale, float* parts,
+embed_sum_kernel(const TokenRecord* rec, const int32_t* total, int32_t windows, int32_t window, int32_t slices,
+                 const S* dout, int64_t dout_ld, D* dtable, int64_t ld, int64_t dim, float scale, float* parts,
                  uint32_t* arrived) {
     chain_wait();
     const int32_t n = *after_wait(total);
@@ -325,7 +327,8 @@ embed_sum_kernel(const TokenRecord* rec, const int32_t* total, int32_t windows, 
                     if (lane == 0) before = atomicAdd(arrived + static_cast<int64_t>(w0) * slices + slice, 1u);
                     if (__shfl_sync(~0u, before, 0) == static_cast<uint32_t>(w1 - w0)) {
                         __threadfence();
-                        join_parts<D, ADD, VEC, SUB>(parts, w0, w1, base, dim, dtable + static_cast<int64_t>(row) * ld, scale);
+                        join_parts<D, ADD, VEC, SUB>(parts, w0, w1, base, dim, dtable + static_cast<int64_t>(row) * ld,
+                                                     scale);
                     }
                 }
 #pragma unroll
@@ -438,8 +441,9 @@ cudaError_t sums(const malt_embed_t* e, const Workspace& w, uint8_t* ws, cudaStr
     const int64_t blocks = (windows * slices + kWarps - 1) / kWarps;
     if (blocks >= (int64_t{1} << 31)) return cudaErrorInvalidValue;
     return launch_chained(embed_sum_kernel<S, D, ADD, VEC, SUB>, static_cast<unsigned>(blocks), kThreads, 0, s,
-                          reinterpret_cast<const TokenRecord*>(ws + w.rec), reinterpret_cast<const int32_t*>(ws + w.total),
-                          windows, window, static_cast<int32_t>(slices), static_cast<const S*>(e->rows), e->rows_ld,
+                          reinterpret_cast<const TokenRecord*>(ws + w.rec),
+                          reinterpret_cast<const int32_t*>(ws + w.total), windows, window,
+                          static_cast<int32_t>(slices), static_cast<const S*>(e->rows), e->rows_ld,
                           static_cast<D*>(e->table), e->table_ld, e->dim, e->scale,
                           reinterpret_cast<float*>(ws + w.parts), reinterpret_cast<uint32_t*>(ws + w.arrived));
 }
@@ -492,9 +496,11 @@ int malt_embed_backward(const malt_embed_t* e, int32_t accumulate, void* workspa
     uint8_t* const ws = static_cast<uint8_t*>(workspace);
     nvtxRangePushA("malt_embed_backward");
     const bool tb = e->table_dtype == MALT_BF16, rb = e->rows_dtype == MALT_BF16, add = accumulate != 0;
-    const bool i32 = e->ids_dtype == MALT_I32;
-    cudaError_t c = i32 ? (tb ? sort_types<int32_t, bf16>(e, w, ws, add, s) : sort_types<int32_t, float>(e, w, ws, add, s))
-                        : (tb ? sort_types<int64_t, bf16>(e, w, ws, add, s) : sort_types<int64_t, float>(e, w, ws, add, s));
+    cudaError_t c;
+    if (e->ids_dtype == MALT_I32)
+        c = tb ? sort_types<int32_t, bf16>(e, w, ws, add, s) : sort_types<int32_t, float>(e, w, ws, add, s);
+    else
+        c = tb ? sort_types<int64_t, bf16>(e, w, ws, add, s) : sort_types<int64_t, float>(e, w, ws, add, s);
     if (c == cudaSuccess && e->tokens > 0)
         c = rb ? (tb ? sums_types<bf16, bf16>(e, w, ws, add, s) : sums_types<bf16, float>(e, w, ws, add, s))
                : (tb ? sums_types<float, bf16>(e, w, ws, add, s) : sums_types<float, float>(e, w, ws, add, s));

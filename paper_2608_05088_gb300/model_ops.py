@@ -317,6 +317,7 @@ def distill_loss_grad(logits, top_ids, top_logits, weight=None, temperature: flo
     loss = _loss(logits)
     dlogits = _like("dlogits", dlogits, logits)
     ld = _row_stride("dlogits", dlogits, logits.shape[-1])
-    _check(malt.load().malt_distill_forward_backward(d, loss.data_ptr(), 0, dlogits.data_ptr(), ld,
-                                                     _stream(dev, stream, loss, dlogits)), "malt_distill_forward_backward")
+    raw = _stream(dev, stream, loss, dlogits)
+    _check(malt.load().malt_distill_forward_backward(d, loss.data_ptr(), 0, dlogits.data_ptr(), ld, raw),
+           "malt_distill_forward_backward")
     return loss, dlogits

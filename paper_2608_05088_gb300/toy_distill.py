@@ -80,13 +80,15 @@ class Model:
                        "q_gain": torch.ones(hd).cuda(), "k_gain": torch.ones(hd).cuda()}
         self.grads = {n: torch.zeros_like(w) for n, w in (self.matrices | self.others).items()}
         bf16 = cfg.dtype == torch.bfloat16
-        self.copies = {n: w.to(cfg.dtype) if bf16 else w for n, w in (self.matrices | {"table": self.others["table"]}).items()}
+        copied = self.matrices | {"table": self.others["table"]}
+        self.copies = {n: w.to(cfg.dtype) if bf16 else w for n, w in copied.items()}
         vec = lambda n: torch.empty(n, device="cuda")
         mats = [(w, self.grads[n], torch.empty_like(w), vec(w.shape[0]), vec(w.shape[1]))
                 for n, w in self.matrices.items()]
         rest = [(w, self.copies[n] if bf16 and n == "table" else None, self.grads[n], torch.empty_like(w),
                  torch.empty_like(w), 0.1 if n == "table" else 0.0) for n, w in self.others.items()]
-        self.optimizer = malt.WholeOptimizer(mats, rest, copies=[self.copies[n] for n in self.matrices] if bf16 else None)
+        mat_copies = [self.copies[n] for n in self.matrices] if bf16 else None
+        self.optimizer = malt.WholeOptimizer(mats, rest, copies=mat_copies)
         angle = torch.arange(cfg.seq)[:, None] * 100.0 ** (-torch.arange(hd // 2) / (hd // 2))[None, :]
         self.cos, self.sin = angle.cos().cuda(), angle.sin().cuda()
 

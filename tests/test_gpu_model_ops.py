@@ -532,6 +532,22 @@ def test_distill_gradient(case):
     assert torch.equal(c.x, got)
 
 
+@pytest.mark.parametrize("dtype", ("f32", "bf16"))
+@pytest.mark.parametrize("tau", (1e-2, 1e-4, 1e-7, 1e-12))
+def test_distill_at_cold_temperatures(tau, dtype):
+    """Exponents of any size: s / T reaches 1e14, and softmax is all but the largest entry."""
+    torch, ops = torch_and_ops()
+    c = DistillCase((6, 2500, 20, dtype, "f32", "i32", tau, "any", 0, 0, 0, 0))
+    loss, dx = ops.distill_loss_grad(c.x, c.top_ids, c.t, weight=c.w, temperature=c.tau)
+    want_loss, want_stats, want = c.oracle()
+    bound_loss, bound_stats, bound = c.bounds()
+    check(loss, want_loss, bound_loss, "loss")
+    check(dx, want, out_bound(want, bound, c.dt), "dlogits")
+    again, stats = ops.distill_loss(c.x, c.top_ids, c.t, weight=c.w, temperature=c.tau)
+    check(stats, want_stats, bound_stats, "stats")
+    assert torch.equal(ops.distill_grad(c.x, c.top_ids, c.t, stats, weight=c.w, temperature=c.tau), dx)
+
+
 def test_distill_of_any_weight_and_shape():
     torch, ops = torch_and_ops()
     g = torch.Generator(device="cuda").manual_seed(3)
