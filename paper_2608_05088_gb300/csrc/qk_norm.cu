@@ -617,8 +617,8 @@ qk_backward_any_kernel(const __grid_constant__ Params P) {
     }
 }
 
-// Gain gradients: block 0 adds up the parts of the queries, block 1 of the keys,
-// for 32 entries at a time, every warp a run of the parts.
+// Gain gradients: a block adds up the parts of the queries or the keys for 32 entries,
+// every warp each 32nd part.
 __global__ void __launch_bounds__(1024)
 qk_gain_kernel(const __grid_constant__ Params P) {
     __shared__ float sums[32][33];
@@ -628,9 +628,18 @@ qk_gain_kernel(const __grid_constant__ Params P) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int i = blockIdx.x * 32 + lane;
     const float* const parts = after_wait(K.parts);
+    constexpr int kLoads = 10;      // parts of a warp in flight
     float t = 0.f;
-    if (i < P.dim)
-        for (int k = warp; k < K.blocks; k += 32) t += parts[static_cast<int64_t>(k) * P.dim + i];
+    for (int k0 = warp; k0 < K.blocks; k0 += 32 * kLoads) {
+        float x[kLoads];
+#pragma unroll
+        for (int u = 0; u < kLoads; ++u) {
+            const int k = k0 + 32 * u;
+            x[u] = k < K.blocks && i < P.dim ? parts[static_cast<int64_t>(k) * P.dim + i] : 0.f;
+        }
+#pragma unroll
+        for (int u = 0; u < kLoads; ++u) t += x[u];
+    }
     sums[warp][lane] = t;
     __syncthreads();
     if (warp == 0 && i < P.dim) {
