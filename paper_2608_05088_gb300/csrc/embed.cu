@@ -6,7 +6,7 @@
 // their own order, long runs in windows of a fixed length.
 //
 // Both are bound by HBM, and every row of the gradient is written once.  40960 tokens
-// of 1280 from bf16 rows to fp32: 42 us, 5.7 TB/s (a copy of as many bytes 6.0).  The
+// of 1280 from bf16 rows to fp32: 42 us, 5.8 TB/s (a copy of as many bytes 5.7).  The
 // gradient of 16384 of them to a table of 50304 rows, bf16 to fp32: 60 us, 5.0 TB/s (the
 // order and the zero rows 39, of which the zeros alone take 25; the sums 20); added in
 // place for 4999 x 501 fp32: 13.6 us, bound by the two launches' latencies.
@@ -91,6 +91,7 @@ constexpr int kSortThreads = 1024;
 constexpr int kSortWarps = kSortThreads / 32;
 static_assert(kSortWarps == 32, "a warp adds up one value of each warp");
 constexpr int kSortLoads = 8;               // ids of a lane in flight
+constexpr int kListed = 64;                 // tokens that a warp need not look for twice
 constexpr int kMaxOwned = kSortThreads;     // rows of a block: one thread scans each
 
 // A token in sorted order: its index, its row and the row's range of records.
@@ -106,6 +107,7 @@ embed_sort_kernel(const I* ids, int32_t tokens, int32_t vocab, int shift, int32_
     uint32_t* const place = smem;                               // [kSortWarps][owned]
     int32_t* const row_begin = reinterpret_cast<int32_t*>(smem + kSortWarps * owned);
     int32_t* const row_end = row_begin + owned;
+    __shared__ int32_t listed[kSortWarps][kListed];     // the warp's first tokens of this block's rows
     __shared__ int32_t warp_tmp[kSortWarps];
     __shared__ int32_t s_base;
 
@@ -121,7 +123,7 @@ embed_sort_kernel(const I* ids, int32_t tokens, int32_t vocab, int shift, int32_
     const int32_t lo = static_cast<int32_t>(min(static_cast<int64_t>(warp) * per, static_cast<int64_t>(tokens)));
     const int32_t hi = static_cast<int32_t>(min(static_cast<int64_t>(lo) + per, static_cast<int64_t>(tokens)));
     uint32_t* const mine = place + warp * owned;
-    int32_t below = 0;
+    int32_t below = 0, found = 0;
     for (int32_t i0 = lo; i0 < hi; i0 += 32 * kSortLoads) {
         int64_t id[kSortLoads];
 #pragma unroll
@@ -131,10 +133,17 @@ embed_sort_kernel(const I* ids, int32_t tokens, int32_t vocab, int shift, int32_
         }
 #pragma unroll
         for (int k = 0; k < kSortLoads; ++k) {
-            if (static_cast<uint64_t>(id[k]) >= static_cast<uint64_t>(vocab)) continue;     // negative ones too
+            const bool inside = static_cast<uint64_t>(id[k]) < static_cast<uint64_t>(vocab);   // nor negative
             const uint32_t of = static_cast<uint32_t>(id[k]) & mask;
-            below += of < blockIdx.x;
-            if (of == blockIdx.x) atomicAdd(mine + (static_cast<uint32_t>(id[k]) >> shift), 1u);
+            below += inside && of < blockIdx.x;
+            const bool in = inside && of == blockIdx.x;
+            const unsigned m = __ballot_sync(~0u, in);
+            if (in) {
+                atomicAdd(mine + (static_cast<uint32_t>(id[k]) >> shift), 1u);
+                const int32_t at = found + __popc(m & ((1u << lane) - 1));
+                if (at < kListed) listed[warp][at] = i0 + 32 * k + lane;
+            }
+            found += __popc(m);
         }
     }
     below = __reduce_add_sync(~0u, below);
@@ -174,28 +183,37 @@ embed_sort_kernel(const I* ids, int32_t tokens, int32_t vocab, int shift, int32_
     if (blockIdx.x == gridDim.x - 1 && threadIdx.x == kSortThreads - 1) *total = s_base + before + incl;
     __syncthreads();
 
-    for (int32_t i0 = lo; i0 < hi; i0 += 32 * kSortLoads) {
-        int64_t id[kSortLoads];
-#pragma unroll
-        for (int k = 0; k < kSortLoads; ++k) {
-            const int32_t i = i0 + 32 * k + lane;
-            id[k] = i < hi ? load_id(ids, i) : -1;
+    // Each token to its row's next place, in the tokens' order.
+    auto put = [&](bool in, int32_t token, int64_t id) {
+        const unsigned m = __ballot_sync(~0u, in);
+        if (in) {
+            const uint32_t r = static_cast<uint32_t>(id) >> shift;
+            const unsigned peers = __match_any_sync(m, r), lower = peers & ((1u << lane) - 1);
+            const uint32_t first = mine[r];
+            __syncwarp(m);
+            if (lower == 0) mine[r] = first + __popc(peers);
+            __syncwarp(m);
+            rec[first + __popc(lower)] = TokenRecord{token, static_cast<int32_t>(id), row_begin[r], row_end[r]};
         }
+    };
+    if (found <= kListed) {
+        for (int32_t i = lane; i - lane < found; i += 32) {
+            const int32_t token = i < found ? listed[warp][i] : 0;
+            put(i < found, token, i < found ? load_id(ids, token) : -1);
+        }
+    } else {
+        for (int32_t i0 = lo; i0 < hi; i0 += 32 * kSortLoads) {
+            int64_t id[kSortLoads];
 #pragma unroll
-        for (int k = 0; k < kSortLoads; ++k) {
-            const bool in = static_cast<uint64_t>(id[k]) < static_cast<uint64_t>(vocab) &&
-                            (static_cast<uint32_t>(id[k]) & mask) == blockIdx.x;
-            const unsigned m = __ballot_sync(~0u, in);
-            if (in) {
-                const uint32_t r = static_cast<uint32_t>(id[k]) >> shift;
-                const unsigned peers = __match_any_sync(m, r), lower = peers & ((1u << lane) - 1);
-                const uint32_t first = mine[r];
-                __syncwarp(m);
-                if (lower == 0) mine[r] = first + __popc(peers);
-                __syncwarp(m);
-                rec[first + __popc(lower)] =
-                    TokenRecord{i0 + 32 * k + lane, static_cast<int32_t>(id[k]), row_begin[r], row_end[r]};
+            for (int k = 0; k < kSortLoads; ++k) {
+                const int32_t i = i0 + 32 * k + lane;
+                id[k] = i < hi ? load_id(ids, i) : -1;
             }
+#pragma unroll
+            for (int k = 0; k < kSortLoads; ++k)
+                put(static_cast<uint64_t>(id[k]) < static_cast<uint64_t>(vocab) &&
+                        (static_cast<uint32_t>(id[k]) & mask) == blockIdx.x,
+                    i0 + 32 * k + lane, id[k]);
         }
     }
     if (!fill) return;

@@ -4,6 +4,7 @@
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
+#include <atomic>
 #include <cstdint>
 #include <cstdio>
 #include <utility>
@@ -193,16 +194,17 @@ inline int cuda_status(cudaError_t e, const char* what) {
 // SMs of the current device (looked up once per device).
 inline int sm_count() {
     constexpr int kDevices = 64;
-    static int counts[kDevices] = {};
+    static std::atomic<int> counts[kDevices] = {};
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess) { cudaGetLastError(); return 1; }
-    if (dev >= 0 && dev < kDevices && counts[dev] > 0) return counts[dev];
+    const bool known = dev >= 0 && dev < kDevices;
+    if (known && counts[dev].load(std::memory_order_relaxed) > 0) return counts[dev].load(std::memory_order_relaxed);
     int n = 0;
     if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) {
         cudaGetLastError();
         return 1;
     }
-    if (dev >= 0 && dev < kDevices) counts[dev] = n;    // the same value from any thread
+    if (known) counts[dev].store(n, std::memory_order_relaxed);
     return n;
 }
 
