@@ -40,15 +40,18 @@ constexpr int kMaxTop = 1024;
 // sweep to the second (8192 rows of 50304 bf16: 251 us, medium 343).  Medium: single
 // sweeps, and both sweeps of parts up to kMediumPart, whose blocks spend their time at
 // barriers (16384 rows of 8192 bf16: 105 us, wide 175; 8000 of 16384 fp32: 218, wide
-// 157).  Narrow: rows up to kNarrowRow (16384 of 2000 bf16: 53 us, medium 74).
+// 157).  Short and narrow: more rows at a time, for rows whose time is latency (16384 of
+// 8192 bf16: short 88 us; 6000 of 16384: short 76, medium 68; 16384 of 4000: narrow 49,
+// short 55; of 2000: narrow 34, 46 at 96 threads).
 struct Shape {
     int threads, blocks, batch;
 };
-enum Width { kNarrow, kMedium, kWide };
+enum Width { kNarrow, kShort, kMedium, kWide };
 __host__ __device__ constexpr Shape shape_of(int width) {
-    return width == kNarrow ? Shape{96, 10, 4} : width == kMedium ? Shape{224, 7, 4} : Shape{480, 3, 5};
+    return width == kNarrow ? Shape{64, 20, 4} : width == kShort ? Shape{128, 12, 4}
+         : width == kMedium ? Shape{224, 7, 4} : Shape{480, 3, 5};
 }
-constexpr int64_t kNarrowRow = 6 * 1024, kMediumPart = 56 * 1024;
+constexpr int64_t kNarrowRow = 9 * 1024, kShortRow = 17 * 1024, kMediumPart = 56 * 1024;
 // Bytes of a row that one block takes, at most, in clusters of up to kSizeCluster.  With
 // a forward sweep larger parts push one another out of L2 (2048 rows of 131072 bf16: two
 // parts 198 us, one 233), smaller ones wait for one another.  The gradient alone waits
@@ -378,6 +381,7 @@ struct Part {
 template <typename T, bool FWD, bool GRAD, bool SAME, int WIDTH>
 __global__ void __launch_bounds__(shape_of(WIDTH).threads + 32, shape_of(WIDTH).blocks)
 distill_kernel(const __grid_constant__ Params P) {
+    static_assert(shape_of(WIDTH).threads >= 64, "a row's odd entries fall to threads 0..7 and 32..39");
     constexpr int N = shape_of(WIDTH).threads, kBatch = shape_of(WIDTH).batch;
     namespace cg = cooperative_groups;
     constexpr int VEC = 16 / sizeof(T), kWarps = N / 32, kAll = N + 32;
@@ -527,6 +531,7 @@ cudaError_t launch(const malt_distill_t* d, const Params& P, cudaStream_t s) {
     // Short rows leave most of a wide block waiting for its barriers; a single sweep has
     // nothing to keep in L2.
     if (bytes <= kNarrowRow) return launch_width<T, FWD, GRAD, kNarrow>(d, P, parts, s);
+    if (bytes <= kShortRow) return launch_width<T, FWD, GRAD, kShort>(d, P, parts, s);
     if constexpr (FWD && GRAD)
         if (bytes / parts > kMediumPart) return launch_width<T, FWD, GRAD, kWide>(d, P, parts, s);
     return launch_width<T, FWD, GRAD, kMedium>(d, P, parts, s);
