@@ -55,9 +55,10 @@ constexpr int64_t kNarrowRow = 9 * 1024, kShortRow = 17 * 1024, kMediumPart = 56
 // Bytes of a row that one block takes, at most, in clusters of up to kSizeCluster.  With
 // a forward sweep larger parts push one another out of L2 (2048 rows of 131072 bf16: two
 // parts 198 us, one 233), smaller ones wait for one another.  The gradient alone waits
-// for nothing, and small parts fill the last wave (1531 fp32 rows of 50257: 104 us at 70
-// KB, 112 at 140).  Clusters of 8 leave more SMs without one (300 fp32 rows of 150000: 88
-// us, 75 in fours).
+// for nothing, needs no clusters (104 us with them for 102), and small parts fill the
+// last wave (1531 fp32 rows of 50257: 102 us at 70 KB, 104 at 140; 8192 bf16 rows of
+// 50304: 253 and 264).  Clusters of 8 leave more SMs without one (300 fp32 rows of
+// 150000: 88 us, 75 in fours).
 constexpr int64_t kSweptPart = 140 * 1024, kWrittenPart = 70 * 1024;
 constexpr int kSizeCluster = 4;
 // While a row's blocks leave SMs idle: up to the largest portable cluster.
@@ -79,6 +80,7 @@ struct Params {
     const float* dloss;         // gradient: d (the caller's value) / d loss, or null for 1
     void* dlogits;
     int64_t dlogits_ld;
+    int32_t parts;              // blocks of a row: with a forward sweep a cluster
 };
 
 // Max and sum of 2^((x - max) c) of a set of values.
@@ -390,7 +392,8 @@ distill_kernel(const __grid_constant__ Params P) {
     __shared__ int listed;
     extern __shared__ uint4 entries[];      // the teacher's
     const cg::cluster_group cluster = cg::this_cluster();
-    const int parts = static_cast<int>(cluster.num_blocks()), part = static_cast<int>(cluster.block_rank());
+    const int parts = FWD ? static_cast<int>(cluster.num_blocks()) : P.parts;
+    const int part = FWD ? static_cast<int>(cluster.block_rank()) : static_cast<int>(blockIdx.x & (parts - 1));
     const int64_t row = blockIdx.x / parts;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const bool teacher = warp == kWarps;
@@ -509,13 +512,14 @@ int check(const malt_distill_t* d) {
 int64_t entries_bytes(int64_t top) { return 16 * padded_top(static_cast<int>(top)); }
 
 template <typename T, bool FWD, bool GRAD, int WIDTH>
-cudaError_t launch_width(const malt_distill_t* d, const Params& P, int parts, cudaStream_t s) {
+cudaError_t launch_width(const malt_distill_t* d, Params P, int parts, cudaStream_t s) {
     constexpr int V = 16 / sizeof(T);
+    P.parts = parts;
     auto past = [](const void* p) { return reinterpret_cast<uintptr_t>(p) % 16; };
     const bool same = !GRAD || (past(P.logits) == past(P.dlogits) && (P.ld - P.dlogits_ld) % V == 0);
     return launch_clusters(same ? distill_kernel<T, FWD, GRAD, true, WIDTH>
                                 : distill_kernel<T, FWD, GRAD, !GRAD, WIDTH>,
-                           static_cast<unsigned>(d->rows * parts), parts, shape_of(WIDTH).threads + 32,
+                           static_cast<unsigned>(d->rows * parts), FWD ? parts : 1, shape_of(WIDTH).threads + 32,
                            entries_bytes(d->top), s, P);
 }
 
