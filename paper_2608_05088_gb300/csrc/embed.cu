@@ -195,6 +195,7 @@ embed_sort_kernel(const I* ids, int32_t tokens, int32_t vocab, int shift, int32_
             __syncwarp(m);
             rec[first + __popc(lower)] = TokenRecord{token, static_cast<int32_t>(id), row_begin[r], row_end[r]};
         }
+        __syncwarp();       // the next call's lanes may be others: votes order no memory
     };
     if (found <= kListed) {
         for (int32_t i = lane; i - lane < found; i += 32) {
