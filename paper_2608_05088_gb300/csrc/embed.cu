@@ -346,6 +346,7 @@ embed_sum_kernel(const TokenRecord* rec, const int32_t* total, int32_t windows, 
                     if (lane == 0) before = atomicAdd(arrived + static_cast<int64_t>(w0) * slices + slice, 1u);
                     if (__shfl_sync(~0u, before, 0) == static_cast<uint32_t>(w1 - w0)) {
                         __threadfence();
+                        __syncwarp();       // the lanes' loads after the lane that saw the count
                         join_parts<D, ADD, VEC, SUB>(parts, w0, w1, base, dim, dtable + static_cast<int64_t>(row) * ld,
                                                      scale);
                     }

@@ -24,3 +24,18 @@ def test_every_token_of_crowded_rows_is_placed_once(per_warp, rows):
         added = torch.ones(vocab, dim, device="cuda")
         ops.embed_grad(dout.cuda(), at, vocab, out=added, accumulate=True)
         assert torch.equal(added.cpu(), want + 1)
+
+
+@pytest.mark.parametrize("dim", (128, 1280, 77))
+def test_parts_of_long_rows_are_this_calls(dim):
+    """Rows over many windows, gradients of changing whole numbers in memory that the call before
+    left full of other parts: a part read too early changes a sum."""
+    import torch
+    from paper_2608_05088_gb300 import model_ops as ops
+    tokens = 6000
+    g = torch.Generator().manual_seed(dim)
+    ids = torch.randint(0, 5, (tokens,), generator=g).cuda()
+    douts = [torch.randint(-8, 9, (tokens, dim), generator=g).float().cuda() for _ in range(2)]
+    want = [torch.zeros(5, dim, device="cuda", dtype=torch.float64).index_add_(0, ids, d.double()) for d in douts]
+    for i in range(20):
+        assert torch.equal(ops.embed_grad(douts[i % 2], ids, 5).double(), want[i % 2])
