@@ -7,8 +7,8 @@ that the library cannot take), allocates what it returns unless an output is
 given, and enqueues the library's kernels on `stream` (default: the current one)
 without synchronising.  Tensors live on the current CUDA device; only the last
 dimension has to be contiguous where nothing else is said.  With a `stream` other
-than the current one, the caller orders its inputs and the use of its outputs; memory
-allocated here is marked as used on that stream.
+than the current one, the caller orders its inputs and the use of its outputs; what is
+allocated here belongs to that stream, and results may be dropped at any time.
 
 For a few tokens the time of a call is the host's, so the checks read each property
 of a tensor once, the current device and stream come from torch._C, without the Python
@@ -54,15 +54,17 @@ def _device(names, *tensors):
     return dev
 
 
-def _stream(dev, stream, *allocated):
-    """The raw stream; memory allocated for this call is kept for it."""
-    current = _current_stream(dev)
-    if stream is None or stream.cuda_stream == current:
-        return current
-    for t in allocated:
+def _on(stream, op, *args):
+    """op(*args) with `stream` as the current one.  What the call allocates is then free for reuse
+    in that stream's order; its results are kept until both streams are done with them."""
+    caller = torch.cuda.current_stream()
+    with torch.cuda.stream(stream):
+        results = op(*args)
+    for t in results if isinstance(results, tuple) else (results,):
         if t is not None:
+            t.record_stream(caller)
             t.record_stream(stream)
-    return stream.cuda_stream
+    return results
 
 
 def _float_code(name, t):
@@ -107,6 +109,8 @@ def embed(table, ids, scale: float = 1.0, dtype=None, out=None, stream=None):
     """scale * table[ids], of shape ids.shape + (dim,) in `dtype` (default: the
     table's).  A negative id is padding (a zero row); an id past the table gives
     a NaN row.  ids must be contiguous."""
+    if stream is not None:
+        return _on(stream, embed, table, ids, scale, dtype, out)
     dev = _device("table ids out", table, ids, out)
     if table.dim() != 2:
         raise ValueError("table must be a vocab x dim matrix")
@@ -121,7 +125,7 @@ def embed(table, ids, scale: float = 1.0, dtype=None, out=None, stream=None):
     e = _EMBED.pack(ids.data_ptr(), _index_code("ids", ids), _float_code("table", table), _float_code("out", out),
                     scale, ids.numel(), vocab, dim, table.data_ptr(), _row_stride("table", table, dim),
                     out.data_ptr(), _row_stride("out", out, dim))
-    _check(malt.load().malt_embed_forward(e, _stream(dev, stream, out)), "malt_embed_forward")
+    _check(malt.load().malt_embed_forward(e, _current_stream(dev)), "malt_embed_forward")
     return out
 
 
@@ -131,6 +135,8 @@ def embed_grad(dout, ids, vocab: int, scale: float = 1.0, dtype=None, out=None, 
     id is v.  Returns a vocab x dim matrix in `dtype` (default: float32), every row
     written; with `accumulate` the sums are added to `out` instead (only rows that
     occur are touched)."""
+    if stream is not None:
+        return _on(stream, embed_grad, dout, ids, vocab, scale, dtype, out, accumulate)
     dev = _device("dout ids out", dout, ids, out)
     if not ids.is_contiguous():
         raise ValueError("ids must be contiguous")
@@ -150,7 +156,7 @@ def embed_grad(dout, ids, vocab: int, scale: float = 1.0, dtype=None, out=None, 
     e = _EMBED.pack(ids.data_ptr(), _index_code("ids", ids), _float_code("out", out), _float_code("dout", dout),
                     scale, n, vocab, dim, out.data_ptr(), _row_stride("out", out, dim),
                     dout.data_ptr(), _row_stride("dout", dout, dim))
-    _check(lib.malt_embed_backward(e, 1 if accumulate else 0, ws.data_ptr(), size, _stream(dev, stream, out, ws)),
+    _check(lib.malt_embed_backward(e, 1 if accumulate else 0, ws.data_ptr(), size, _current_stream(dev)),
            "malt_embed_backward")
     return out
 
@@ -223,12 +229,14 @@ def qk_norm(q, k, q_gain, k_gain, cos, sin, positions=None, eps: float = 1e-6, i
     dimension; cos, sin: [positions, pairs]; positions: [batch, seq] or [seq] ([tokens]),
     default 0 .. seq-1.  Pairs are (i, pairs + i), or (2i, 2i+1) when interleaved.
     Returns (q_out, k_out); each may be given, also as its input itself."""
+    if stream is not None:
+        return _on(stream, qk_norm, q, k, q_gain, k_gain, cos, sin, positions, eps, interleaved, q_out, k_out)
     dev = _device("q k q_gain k_gain cos sin positions q_out k_out", q, k, q_gain, k_gain, cos, sin, positions, q_out,
                   k_out)
     p = _qk_params(q, k, q_gain, k_gain, cos, sin, positions, eps, interleaved)
     q_out, k_out = _like("q_out", q_out, q), _like("k_out", k_out, k)
     _check(malt.load().malt_qk_norm_forward(p, _heads(q), _heads(k), _heads(q_out), _heads(k_out),
-                                            _stream(dev, stream, q_out, k_out)), "malt_qk_norm_forward")
+                                            _current_stream(dev)), "malt_qk_norm_forward")
     return q_out, k_out
 
 
@@ -237,6 +245,9 @@ def qk_norm_grad(dq_out, dk_out, q, k, q_gain, k_gain, cos, sin, positions=None,
     """The gradient of qk_norm from those of its outputs and its own arguments.  Returns
     (dq, dk, dq_gain, dk_gain), the gains' gradients in float32 (None for a gain that is None); dq
     and dk may be given, also as dq_out and dk_out themselves."""
+    if stream is not None:
+        return _on(stream, qk_norm_grad, dq_out, dk_out, q, k, q_gain, k_gain, cos, sin, positions, eps, interleaved,
+                   dq, dk)
     dev = _device("q k dq_out dk_out q_gain k_gain cos sin positions dq dk", q, k, dq_out, dk_out, q_gain, k_gain, cos,
                   sin, positions, dq, dk)
     p = _qk_params(q, k, q_gain, k_gain, cos, sin, positions, eps, interleaved)
@@ -251,7 +262,7 @@ def qk_norm_grad(dq_out, dk_out, q, k, q_gain, k_gain, cos, sin, positions=None,
     ws = torch.empty(size, dtype=torch.uint8, device=q.device)
     _check(lib.malt_qk_norm_backward(p, _heads(dq_out), _heads(dk_out), _heads(q), _heads(k), _heads(dq), _heads(dk),
                                      _pointer(dq_gain), _pointer(dk_gain), ws.data_ptr(), size,
-                                     _stream(dev, stream, dq, dk, dq_gain, dk_gain, ws)), "malt_qk_norm_backward")
+                                     _current_stream(dev)), "malt_qk_norm_backward")
     return dq, dk, dq_gain, dk_gain
 
 
@@ -283,11 +294,13 @@ def distill_loss(logits, top_ids, top_logits, weight=None, temperature: float = 
     statistics [rows, 2] that distill_grad takes.  Entries with an id outside the
     vocabulary or a logit of -inf are not listed; rows of weight 0 or with nothing
     listed have loss 0."""
+    if stream is not None:
+        return _on(stream, distill_loss, logits, top_ids, top_logits, weight, temperature)
     dev = _device("logits top_ids top_logits weight", logits, top_ids, top_logits, weight)
     d = _distill_params(logits, top_ids, top_logits, weight, temperature)
     loss = _loss(logits)
     stats = torch.empty((loss.numel(), 2), dtype=torch.float32, device=logits.device)
-    _check(malt.load().malt_distill_forward(d, loss.data_ptr(), stats.data_ptr(), _stream(dev, stream, loss, stats)),
+    _check(malt.load().malt_distill_forward(d, loss.data_ptr(), stats.data_ptr(), _current_stream(dev)),
            "malt_distill_forward")
     return loss, stats
 
@@ -296,6 +309,8 @@ def distill_grad(logits, top_ids, top_logits, stats, dloss=None, weight=None, te
                  dlogits=None, stream=None):
     """The gradient of the logits from distill_loss's statistics and the gradient of each row's
     loss (None: ones), in the logits' type; dlogits may be given, also as the logits."""
+    if stream is not None:
+        return _on(stream, distill_grad, logits, top_ids, top_logits, stats, dloss, weight, temperature, dlogits)
     dev = _device("logits top_ids top_logits weight stats dloss dlogits", logits, top_ids, top_logits, weight, stats,
                   dloss, dlogits)
     d = _distill_params(logits, top_ids, top_logits, weight, temperature)
@@ -305,19 +320,20 @@ def distill_grad(logits, top_ids, top_logits, stats, dloss=None, weight=None, te
     dlogits = _like("dlogits", dlogits, logits)
     ld = _row_stride("dlogits", dlogits, logits.shape[-1])
     _check(malt.load().malt_distill_backward(d, stats.data_ptr(), _pointer(dloss), dlogits.data_ptr(), ld,
-                                             _stream(dev, stream, dlogits)), "malt_distill_backward")
+                                             _current_stream(dev)), "malt_distill_backward")
     return dlogits
 
 
 def distill_loss_grad(logits, top_ids, top_logits, weight=None, temperature: float = 1.0, dlogits=None, stream=None):
     """distill_loss and the gradient of the losses' sum in one pass over the logits (a mean is a
     weight of 1 / rows).  Returns (loss, dlogits); dlogits may be given, also as the logits."""
+    if stream is not None:
+        return _on(stream, distill_loss_grad, logits, top_ids, top_logits, weight, temperature, dlogits)
     dev = _device("logits top_ids top_logits weight dlogits", logits, top_ids, top_logits, weight, dlogits)
     d = _distill_params(logits, top_ids, top_logits, weight, temperature)
     loss = _loss(logits)
     dlogits = _like("dlogits", dlogits, logits)
     ld = _row_stride("dlogits", dlogits, logits.shape[-1])
-    raw = _stream(dev, stream, loss, dlogits)
-    _check(malt.load().malt_distill_forward_backward(d, loss.data_ptr(), 0, dlogits.data_ptr(), ld, raw),
-           "malt_distill_forward_backward")
+    _check(malt.load().malt_distill_forward_backward(d, loss.data_ptr(), 0, dlogits.data_ptr(), ld,
+                                                     _current_stream(dev)), "malt_distill_forward_backward")
     return loss, dlogits

@@ -39,3 +39,58 @@ def test_parts_of_long_rows_are_this_calls(dim):
     want = [torch.zeros(5, dim, device="cuda", dtype=torch.float64).index_add_(0, ids, d.double()) for d in douts]
     for i in range(20):
         assert torch.equal(ops.embed_grad(douts[i % 2], ids, 5).double(), want[i % 2])
+
+
+def _stream_calls(seed):
+    """Every operator on inputs of one seed: calls that take a stream and return a list of results."""
+    import torch
+    from paper_2608_05088_gb300 import model_ops as ops
+    g = torch.Generator("cuda").manual_seed(seed)
+    normal = lambda *s: torch.randn(*s, device="cuda", generator=g)
+    table, ids = normal(4000, 64), torch.randint(0, 40, (900,), device="cuda", generator=g)
+    dout = normal(900, 64)
+    q, k, dq, dk = (normal(2, 150, h, 64) for h in (8, 4, 8, 4))
+    gain, cs = normal(64), normal(150, 32)
+    x = normal(64, 4000)
+    t, top = normal(64, 4000).topk(8, dim=1)
+    stats = ops.distill_loss(x, top, t)[1]
+    torch.cuda.synchronize()
+    return [lambda s: [ops.embed(table, ids, stream=s)],
+            lambda s: [ops.embed_grad(dout, ids, 4000, stream=s)],
+            lambda s: list(ops.qk_norm(q, k, gain, gain, cs, cs, stream=s)),
+            lambda s: list(ops.qk_norm_grad(dq, dk, q, k, gain, gain, cs, cs, stream=s)),
+            lambda s: list(ops.distill_loss(x, top, t, stream=s)),
+            lambda s: [ops.distill_grad(x, top, t, stats, stream=s)],
+            lambda s: list(ops.distill_loss_grad(x, top, t, stream=s))]
+
+
+@pytest.mark.parametrize("op", range(7))
+def test_memory_of_a_call_on_another_stream(op):
+    """Blocks that the current stream freed, its work on them still queued, are of the sizes that
+    the call allocates; and a result dropped while the current stream has yet to read it is not
+    handed to the next call."""
+    import torch
+    from paper_2608_05088_gb300 import malt
+    first, second = _stream_calls(1)[op], _stream_calls(2)[op]
+    want = first(None)
+    side, here = torch.cuda.Stream(), torch.cuda.current_stream()
+    sizes = [t.numel() * t.element_size() for t in want]
+    sizes += [malt.load().malt_embed_workspace_bytes(900, 64), malt.load().malt_qk_norm_workspace_bytes(64)]
+    for _ in range(3):
+        freed = [torch.empty(n, dtype=torch.uint8, device="cuda") for n in sizes for _ in range(4)]
+        torch.cuda.synchronize()
+        torch.cuda._sleep(20_000_000)
+        for t in freed:
+            t.fill_(0x55)       # behind the sleep
+        del freed, t
+        got = first(side)
+        side.synchronize()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+        here.wait_stream(side)
+        torch.cuda._sleep(20_000_000)
+        kept = [t.clone() for t in got]         # behind the sleep
+        del got
+        other = second(side)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(kept, want)) and len(other) == len(want)
