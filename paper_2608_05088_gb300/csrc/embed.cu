@@ -433,11 +433,11 @@ cudaError_t sort(const malt_embed_t* e, const Workspace& w, uint8_t* ws, bool ad
     const int32_t owned = static_cast<int32_t>((e->vocab + blocks - 1) / blocks);
     const size_t smem = (kSortWarps + 2) * sizeof(uint32_t) * static_cast<size_t>(owned);
     auto* const kernel = embed_sort_kernel<I, D, VEC>;
-    if (smem > 48 * 1024) {
-        const cudaError_t rc = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                                    static_cast<int>(smem));
-        if (rc != cudaSuccess) { cudaGetLastError(); return rc; }
-    }
+    // Always, and always the most that a block may own: whether 48 KB are passed depends on
+    // the kernel's static arrays too, and calls of other threads set the same value.
+    constexpr int kMost = (kSortWarps + 2) * static_cast<int>(sizeof(uint32_t)) * kMaxOwned;
+    const cudaError_t rc = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost);
+    if (rc != cudaSuccess) { cudaGetLastError(); return rc; }
     return launch_chained(kernel, static_cast<unsigned>(blocks), kSortThreads, smem, s, static_cast<const I*>(e->ids),
                           static_cast<int32_t>(e->tokens), static_cast<int32_t>(e->vocab), shift, owned,
                           reinterpret_cast<TokenRecord*>(ws + w.rec), reinterpret_cast<int32_t*>(ws + w.total),

@@ -94,3 +94,31 @@ def test_memory_of_a_call_on_another_stream(op):
         other = second(side)
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(kept, want)) and len(other) == len(want)
+
+
+_LARGE_TABLES = """
+import sys, torch
+sys.path.insert(0, {root!r})
+from paper_2608_05088_gb300 import model_ops as ops
+vocab, dim = {vocab}, {dim}
+ids = torch.randint(0, vocab, (300,), generator=torch.Generator().manual_seed(vocab))
+dout = torch.randint(-8, 9, (300, dim), generator=torch.Generator().manual_seed(1)).float()
+want = torch.zeros(vocab, dim).index_add_(0, ids, dout)
+for index in (torch.int32, torch.int64):
+    for table in (torch.float32, torch.bfloat16):
+        got = ops.embed_grad(dout.cuda(), ids.to("cuda", index), vocab, dtype=table)
+        assert torch.equal(got.float().cpu(), want), (index, table)
+"""
+
+
+@pytest.mark.parametrize("dim", (8, 5))
+@pytest.mark.parametrize("vocab", (38400, 38401, 40478, 46208, 46209, 131072, 131073))
+def test_embedding_gradient_of_any_vocabulary_alone(vocab, dim):
+    """In a process of its own: nothing that a call of another size left behind helps this one."""
+    import pathlib
+    import subprocess
+    import sys
+    root = str(pathlib.Path(__file__).resolve().parent.parent)
+    r = subprocess.run([sys.executable, "-c", _LARGE_TABLES.format(root=root, vocab=vocab, dim=dim)],
+                       capture_output=True, text=True, timeout=120)
+    assert r.returncode == 0, r.stderr[-2000:]
