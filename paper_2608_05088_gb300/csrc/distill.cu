@@ -225,7 +225,11 @@ __device__ __forceinline__ void look_up(const Params& P, const T* x, int begin, 
 __device__ __forceinline__ int softmax_of(const Params& P, const Top& top, float inv_tau) {
     const int lane = threadIdx.x & 31;
     float max = -INFINITY, sum = 0.f;
-    for (int j = lane; j < P.top; j += 32) max = fmaxf(max, top.t[j]);
+    bool any = false;           // by the ids: the maximum passes NaN over
+    for (int j = lane; j < P.top; j += 32) {
+        max = fmaxf(max, top.t[j]);
+        any |= top.id[j] >= 0;
+    }
     max = warp_max(max);
     for (int j = lane; j < P.top; j += 32) {
         const float t = (top.t[j] - max) * inv_tau, e = top.id[j] >= 0 ? expf(t) : 0.f;
@@ -239,7 +243,7 @@ __device__ __forceinline__ int softmax_of(const Params& P, const Top& top, float
         top.t[j] -= log_t;
         top.p[j] *= f;
     }
-    return max != -INFINITY;        // listed entries have a larger logit
+    return __any_sync(~0u, any);
 }
 
 // Loss and statistics of a row, by one warp.

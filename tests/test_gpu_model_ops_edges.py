@@ -122,3 +122,28 @@ def test_embedding_gradient_of_any_vocabulary_alone(vocab, dim):
     r = subprocess.run([sys.executable, "-c", _LARGE_TABLES.format(root=root, vocab=vocab, dim=dim)],
                        capture_output=True, text=True, timeout=120)
     assert r.returncode == 0, r.stderr[-2000:]
+
+
+@pytest.mark.parametrize("teacher", ("float32", "bfloat16"))
+@pytest.mark.parametrize("top", (1, 5, 40))
+def test_a_teacher_of_nan_is_listed(top, teacher):
+    """Rows: finite entries; one NaN among them; all NaN; NaN where nothing is listed."""
+    import torch
+    from paper_2608_05088_gb300 import model_ops as ops
+    g = torch.Generator("cuda").manual_seed(top)
+    x = torch.randn(4, 3000, device="cuda", generator=g)
+    ids = torch.rand(4, 3000, device="cuda", generator=g).topk(top, dim=1).indices
+    t = torch.randn(4, top, device="cuda", generator=g)
+    t[1, top // 2] = t[2] = t[3] = float("nan")
+    ids[3] = -1
+    t = t.to(getattr(torch, teacher))
+    loss, stats = ops.distill_loss(x, ids, t)
+    both, dx = ops.distill_loss_grad(x, ids, t)
+    alone = ops.distill_grad(x, ids, t, stats)
+    for got in (loss, both):
+        assert got.isnan().tolist() == [False, True, True, False] and got[3] == 0
+    assert bool((stats[:3] > 0).all()) and not stats[3].any()
+    listed = torch.zeros(4, 3000, dtype=torch.bool, device="cuda")
+    listed[1:3].scatter_(1, ids[1:3], True)
+    for got in (dx, alone):
+        assert torch.equal(got.isnan(), listed) and not got[3].any() and bool((got[1:3][~listed[1:3]] > 0).all())
