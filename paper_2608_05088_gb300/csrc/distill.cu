@@ -136,14 +136,18 @@ __device__ __forceinline__ float largest(const uint4 (&u)[N]) {
 __device__ __forceinline__ bool in_range(float product) { return fabsf(product) < 0x1p20f; }
 
 // Running maximum and sum of a thread, the sum in two halves relative to `ref`, the
-// rounded product m c.
+// rounded product m c, or past the range to m c itself.
 struct Running {
     float m = -INFINITY, ref = -INFINITY;
     f32x2 s = 0;
     __device__ __forceinline__ void raise(float to, float c) {
         if (!(to > m)) return;
         const float next = to * c;
-        const float f = in_range(ref) && in_range(next) ? exp2_fast(ref - next) : exp2_fast((m - to) * c);
+        const bool was = in_range(ref), is = in_range(next);
+        // Past the range the sum is relative to m c itself: on crossing, the rounding of the
+        // side in range comes in.
+        const float f = was && is ? exp2_fast(ref - next)
+                                  : exp2_fast(fmaf(m - to, c, was ? -fmaf(m, c, -ref) : is ? fmaf(to, c, -next) : 0.f));
         s = mul2(s, pack2(f, f));       // from -inf: nothing summed yet, times 0
         m = to;
         ref = next;

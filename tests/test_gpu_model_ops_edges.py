@@ -147,3 +147,58 @@ def test_a_teacher_of_nan_is_listed(top, teacher):
     listed[1:3].scatter_(1, ids[1:3], True)
     for got in (dx, alone):
         assert torch.equal(got.isnan(), listed) and not got[3].any() and bool((got[1:3][~listed[1:3]] > 0).all())
+
+
+@pytest.mark.parametrize("rows,vocab", ((24, 2503), (24, 60000), (160, 1500), (160, 2503), (160, 6000), (160, 20000)))
+@pytest.mark.parametrize("sign", (1, -1))
+@pytest.mark.parametrize("tau", (1.085e-5, 3e-4, 1e-7))
+def test_sums_where_the_maximum_crosses_the_exponents_range(tau, sign, rows, vocab):
+    """Rows of two values a few ulps apart, s / T log2(e) of one below 2^20 in size and of the other
+    not, the lower one first in every thread's order.  Bounds: u for each of the additions in a row
+    (vocab / 512 + 64 at most) and a few of each exponent, which are below 1."""
+    import numpy as np
+    import torch
+    from paper_2608_05088_gb300 import model_ops as ops
+    u, f = 2.0 ** -24, np.float32
+    rng = np.random.default_rng(vocab)
+    tau = float(f(tau))
+    c = f(1.4426950408889634) / f(tau)
+
+    def step(v, n):
+        for _ in range(abs(n)):
+            v = np.nextafter(v, f(np.inf if n > 0 else -np.inf))
+        return v
+
+    edge = f(2.0 ** 20) / c
+    while edge * c < f(2.0 ** 20):
+        edge = step(edge, 1)
+    while step(edge, -1) * c >= f(2.0 ** 20):
+        edge = step(edge, -1)       # the first value past the range
+    x = np.empty((rows, vocab), f)
+    cut = rng.integers(vocab // 3, vocab // 2, rows)
+    for i in range(rows):
+        inside, past = step(edge, -int(rng.integers(1, 5))), step(edge, int(rng.integers(0, 4)))
+        low, high = (inside, past) if sign > 0 else (-past, -inside)
+        x[i, :cut[i]], x[i, cut[i]:] = low, high
+    wide = x.astype(np.float64)
+    m = wide.max(1, keepdims=True)
+    e = np.exp((wide - m) / tau)
+    total = e.sum(1)
+    ids = np.tile([3, vocab - 2], (rows, 1))
+    log_q = (np.take_along_axis(wide, ids, 1) - m) / tau - np.log(total)[:, None]
+    want_loss = tau ** 2 * (0.5 * (np.log(0.5) - log_q)).sum(1)
+    want = e / total[:, None]
+    np.put_along_axis(want, ids, np.take_along_axis(want, ids, 1) - 0.5, 1)
+    rel = (vocab / 512 + 64 + 8) * u
+
+    args = (torch.from_numpy(x).cuda(), torch.from_numpy(ids).cuda(), torch.zeros(rows, 2, device="cuda"))
+    loss, stats = ops.distill_loss(*args, temperature=tau)
+    both, dx = ops.distill_loss_grad(*args, temperature=tau)
+    alone = ops.distill_grad(*args, stats, temperature=tau)
+    host = lambda t: t.double().cpu().numpy()
+    assert (host(stats)[:, 0] == m[:, 0]).all()
+    assert (np.abs(host(stats)[:, 1] / total - 1) <= rel).all()
+    for got in (loss, both):
+        assert (np.abs(host(got) - want_loss) <= tau ** 2 * (rel + 34 * u * (5 + np.abs(log_q).max()))).all()
+    for got in (dx, alone):
+        assert (np.abs(host(got) / tau - want) <= (rel + 24 * u) * e / total[:, None] + 34 * u * (want < 0)).all()
