@@ -10,6 +10,11 @@ dimension has to be contiguous where nothing else is said.  With a `stream` othe
 than the current one, the caller orders its inputs and the use of its outputs; what is
 allocated here belongs to that stream, and results may be dropped at any time.
 
+Results belong to no autograd graph, also those of tensors that require gradients: a
+gradient is a call of its own (an autograd.Function calls it, as toy_distill.py does
+for qk_norm).  An output that is given counts as modified, so that a backward pass
+that has kept it refuses.
+
 For a few tokens the time of a call is the host's, so the checks read each property
 of a tensor once, the current device and stream come from torch._C, without the Python
 objects around them, and outputs come from the cheapest of torch's allocating calls.
@@ -31,6 +36,8 @@ _HEADS = struct.Struct("Pqqqq")
 _DISTILL = struct.Struct("PqqqiiPqPqqPif")
 
 
+# Tells autograd that a tensor changes, for its check of what a backward pass has kept.
+_written = torch.autograd.graph.increment_version
 # The raw handle of a device's current stream, and the current device.
 _current_stream = torch._C._cuda_getCurrentRawStream
 _current_device = torch._C._cuda_getDevice
@@ -122,6 +129,8 @@ def embed(table, ids, scale: float = 1.0, dtype=None, out=None, stream=None):
         out = torch.empty(shape, dtype=table.dtype if dtype is None else dtype, device=table.device)
     elif out.shape != shape or dtype not in (None, out.dtype):
         raise ValueError(f"out has shape {tuple(out.shape)} and dtype {out.dtype}, expected {shape} and {dtype}")
+    else:
+        _written(out)
     e = _EMBED.pack(ids.data_ptr(), _index_code("ids", ids), _float_code("table", table), _float_code("out", out),
                     scale, ids.numel(), vocab, dim, table.data_ptr(), _row_stride("table", table, dim),
                     out.data_ptr(), _row_stride("out", out, dim))
@@ -149,6 +158,8 @@ def embed_grad(dout, ids, vocab: int, scale: float = 1.0, dtype=None, out=None, 
         out = torch.empty((vocab, dim), dtype=torch.float32 if dtype is None else dtype, device=dout.device)
     elif out.shape != (vocab, dim) or dtype not in (None, out.dtype):
         raise ValueError(f"out has shape {tuple(out.shape)} and dtype {out.dtype}, expected {(vocab, dim)} and {dtype}")
+    else:
+        _written(out)
     lib = malt.load()
     n = ids.numel()
     size = lib.malt_embed_workspace_bytes(n, dim)
@@ -172,6 +183,7 @@ def _like(name, t, like):
                          f"and {like.dtype}")
     if 0 in t.stride() and not t.is_contiguous():
         raise ValueError(f"{name} has overlapping entries")
+    _written(t)
     return t
 
 

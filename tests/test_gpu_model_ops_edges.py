@@ -202,3 +202,38 @@ def test_sums_where_the_maximum_crosses_the_exponents_range(tau, sign, rows, voc
         assert (np.abs(host(got) - want_loss) <= tau ** 2 * (rel + 34 * u * (5 + np.abs(log_q).max()))).all()
     for got in (dx, alone):
         assert (np.abs(host(got) / tau - want) <= (rel + 24 * u) * e / total[:, None] + 34 * u * (want < 0)).all()
+
+
+def test_autograd_sees_given_outputs_change():
+    """A tensor that a call writes counts as modified, so a backward pass that has kept it refuses;
+    what the call allocates belongs to no graph."""
+    import torch
+    from paper_2608_05088_gb300 import model_ops as ops
+    new = lambda *s: torch.randn(*s, device="cuda")
+    ids = torch.arange(6, device="cuda")
+    q, gain, cs = new(1, 6, 2, 64), torch.ones(64, device="cuda"), new(6, 32)
+    x = new(6, 100)
+    t, top = x.topk(4, dim=1)
+    stats = ops.distill_loss(x, top, t)[1]
+    calls = [((6, 8), lambda out: ops.embed(new(9, 8), ids, out=out)),
+             ((9, 8), lambda out: ops.embed_grad(new(6, 8), ids, 9, out=out)),
+             ((9, 8), lambda out: ops.embed_grad(new(6, 8), ids, 9, out=out, accumulate=True)),
+             (q.shape, lambda out: ops.qk_norm(q, q, gain, gain, cs, cs, q_out=out)),
+             (q.shape, lambda out: ops.qk_norm(q, q, gain, gain, cs, cs, k_out=out)),
+             (q.shape, lambda out: ops.qk_norm_grad(q, q, q, q, gain, gain, cs, cs, dq=out)),
+             (q.shape, lambda out: ops.qk_norm_grad(q, q, q, q, gain, gain, cs, cs, dk=out)),
+             (x.shape, lambda out: ops.distill_grad(x, top, t, stats, dlogits=out)),
+             (x.shape, lambda out: ops.distill_loss_grad(x, top, t, dlogits=out)),
+             (x.shape, lambda out: ops.distill_loss_grad(out, top, t, dlogits=out)),
+             (x.shape, lambda out: ops.distill_loss_grad(x, top, t, dlogits=out, stream=torch.cuda.Stream()))]
+    for shape, call in calls:
+        y = new(*shape).requires_grad_().sigmoid()          # its gradient is made from y itself
+        torch.cuda.synchronize()
+        call(y.detach())
+        torch.cuda.synchronize()
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            y.sum().backward()
+        with torch.inference_mode():
+            call(new(*shape))
+    table = new(9, 8).requires_grad_()
+    assert not ops.embed(table, ids).requires_grad
