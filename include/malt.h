@@ -477,6 +477,7 @@ typedef struct {
     int64_t     rows_ld;
 } malt_embed_t;
 int malt_embed_forward(const malt_embed_t* e, void* stream);
+/* 0 for sizes that the call refuses. */
 size_t malt_embed_workspace_bytes(int64_t tokens, int64_t dim);
 int malt_embed_backward(const malt_embed_t* e, int32_t accumulate, void* workspace, size_t workspace_bytes,
                         void* stream);

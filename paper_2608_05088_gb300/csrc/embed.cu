@@ -500,7 +500,7 @@ int malt_embed_forward(const malt_embed_t* e, void* stream) {
 }
 
 size_t malt_embed_workspace_bytes(int64_t tokens, int64_t dim) {
-    if (tokens < 0 || dim < 0) return 0;
+    if (tokens < 0 || tokens >= malt::kMaxTokens || dim < 0 || dim > malt::kMaxDim) return 0;
     return malt::workspace_of(tokens, dim).bytes;
 }
 
