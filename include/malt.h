@@ -494,7 +494,8 @@ int malt_embed_backward(const malt_embed_t* e, int32_t accumulate, void* workspa
  * rows, and what the gradient makes of them, are NaN.
  * Each output may be its own input's buffer with the same strides (y = x;
  * dx = dy or dx = x).  head_dim <= 1024, rot_dim even and <= head_dim,
- * batch * seq < 2^31, heads < 2^20 (0 for none). */
+ * batch * seq < 2^31, heads < 2^20 (0 for none), forward batch * seq * heads
+ * < 2^33 - 8. */
 typedef struct {
     int32_t      dtype;                  /* queries, keys, outputs and their gradients */
     int32_t      gain_dtype;

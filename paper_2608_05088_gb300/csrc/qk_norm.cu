@@ -27,6 +27,7 @@ constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
 constexpr int kMaxHeadDim = 1024;
 constexpr int kMaxSplit = 256;
+constexpr int64_t kMaxRows = int64_t{1} << 33;      // of a forward launch, a warp each
 
 struct Rows {           // heads of the tokens of a [batch, seq, heads, dim] view
     void* data;
@@ -808,9 +809,8 @@ cudaError_t forward(Params& P, bool inter, cudaStream_t s) {
     if (const int lanes = lanes_of<T, vector_of<T>()>(P, false))
         return inter ? forward_lanes<T, true>(P, lanes, s) : forward_lanes<T, false>(P, lanes, s);
     for (Kind& K : P.kind) {
-        const int64_t blocks = (P.batch * P.seq * K.heads + kWarps - 1) / kWarps;
-        if (blocks >= (int64_t{1} << 30)) return cudaErrorInvalidValue;
-        K.blocks = static_cast<int32_t>(blocks);
+        static_assert(kMaxRows / kWarps <= int64_t{1} << 30, "the blocks of both kinds are a 32-bit number");
+        K.blocks = static_cast<int32_t>((P.batch * P.seq * K.heads + kWarps - 1) / kWarps);
     }
     return launch_chained(inter ? qk_forward_any_kernel<T, true> : qk_forward_any_kernel<T, false>,
                           P.kind[0].blocks + P.kind[1].blocks, kThreads, 0, s, P);
@@ -846,6 +846,7 @@ int malt_qk_norm_forward(const malt_qk_norm_t* p, const malt_heads_t* q, const m
     const malt_heads_t* const all[4] = {q, k, q_out, k_out};
     for (int i = 0; i < 4; ++i)
         if ((rc = check_heads(p, all[i], i % 2 ? k : q)) != MALT_OK) return rc;
+    if (tokens_of(p) * std::max(q->heads, k->heads) >= kMaxRows - kWarps) return MALT_ERR_UNSUPPORTED;
     if (tokens_of(p) == 0 || q->heads + k->heads == 0) return MALT_OK;
     Params P = params_of(p);
     P.kind[0].x = rows_of(q);

@@ -19,3 +19,11 @@ def test_workspace_of_a_gradient_past_the_limits(lib):
     for tokens, dim in ((1 << 30, 1), (1 << 40, 64), (1, (1 << 24) + 1), (1, 1 << 60)):
         assert lib.malt_embed_workspace_bytes(tokens, dim) == 0
     assert lib.malt_embed_workspace_bytes((1 << 63) - 1, 64) == 0
+
+
+def test_norms_of_too_many_heads_are_unsupported(lib):
+    """2^33 heads of all tokens are past what a launch counts: a size, not an error of CUDA's."""
+    p = model_ops._QK.pack(malt.MALT_F32, malt.MALT_F32, 7, 0, 0, 1e-6, 1, (1 << 31) - 1, 0, 0, 0, 0, A, A, 1, 0, 0)
+    many, few = (model_ops._HEADS.pack(A, n, 0, 7 * n, 7) for n in (8, 0))
+    assert lib.malt_qk_norm_forward(p, many, few, many, few, None) == malt.MALT_ERR_UNSUPPORTED
+    assert lib.malt_qk_norm_forward(p, few, many, few, many, None) == malt.MALT_ERR_UNSUPPORTED
