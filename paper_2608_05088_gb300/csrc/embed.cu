@@ -93,6 +93,8 @@ static_assert(kSortWarps == 32, "a warp adds up one value of each warp");
 constexpr int kSortLoads = 8;               // ids of a lane in flight
 constexpr int kListed = 64;                 // tokens that a warp need not look for twice
 constexpr int kMaxOwned = kSortThreads;     // rows of a block: one thread scans each
+// Bytes of the kernel's static arrays, at most.
+constexpr int kSortStatic = kSortWarps * (kListed + 1) * static_cast<int>(sizeof(int32_t)) + 64;
 
 // A token in sorted order: its index, its row and the row's range of records.
 struct __align__(16) TokenRecord {
@@ -433,11 +435,13 @@ cudaError_t sort(const malt_embed_t* e, const Workspace& w, uint8_t* ws, bool ad
     const int32_t owned = static_cast<int32_t>((e->vocab + blocks - 1) / blocks);
     const size_t smem = (kSortWarps + 2) * sizeof(uint32_t) * static_cast<size_t>(owned);
     auto* const kernel = embed_sort_kernel<I, D, VEC>;
-    // Always, and always the most that a block may own: whether 48 KB are passed depends on
-    // the kernel's static arrays too, and calls of other threads set the same value.
-    constexpr int kMost = (kSortWarps + 2) * static_cast<int>(sizeof(uint32_t)) * kMaxOwned;
-    const cudaError_t rc = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost);
-    if (rc != cudaSuccess) { cudaGetLastError(); return rc; }
+    // Past 48 KB with the kernel's static arrays.  Always to the most that a block may own, so
+    // that calls of other threads set the same value.
+    if (smem + kSortStatic > 48 * 1024) {
+        constexpr int kMost = (kSortWarps + 2) * static_cast<int>(sizeof(uint32_t)) * kMaxOwned;
+        const cudaError_t rc = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost);
+        if (rc != cudaSuccess) { cudaGetLastError(); return rc; }
+    }
     return launch_chained(kernel, static_cast<unsigned>(blocks), kSortThreads, smem, s, static_cast<const I*>(e->ids),
                           static_cast<int32_t>(e->tokens), static_cast<int32_t>(e->vocab), shift, owned,
                           reinterpret_cast<TokenRecord*>(ws + w.rec), reinterpret_cast<int32_t*>(ws + w.total),
