@@ -5,10 +5,14 @@ gradient, and distillation from a teacher's top logits.
 Each function checks its tensors (ValueError for a shape, type, layout or device
 that the library cannot take), allocates what it returns unless an output is
 given, and enqueues the library's kernels on `stream` (default: the current one)
-without synchronising.  Tensors live on the current CUDA device; only the last
-dimension has to be contiguous where nothing else is said.  With a `stream` other
-than the current one, the caller orders its inputs and the use of its outputs; what is
-allocated here belongs to that stream, and results may be dropped at any time.
+without synchronising.  Tensors live on the current CUDA device.  A head, and a row of
+embeddings, logits or teacher's entries, is contiguous; heads may lie at any strides, rows
+at one stride (those of x[..., :n] do, those of x[:, :-1] with three dimensions do not);
+vectors, tables of angles and token ids are contiguous.
+
+With a `stream` other than the current one, the caller orders its inputs and the use of
+its outputs; what is allocated here belongs to that stream, and results may be dropped at
+any time.
 
 Results belong to no autograd graph, also those of tensors that require gradients: a
 gradient is a call of its own (an autograd.Function calls it, as toy_distill.py does
@@ -92,13 +96,21 @@ def _row_stride(name, t, cols):
     """Elements between two rows of t seen as a matrix of its last dimension."""
     if t.is_contiguous():
         return cols
-    if t.dim() != 2 or (cols > 1 and t.stride(1) != 1):
-        raise ValueError(f"{name} must be contiguous, or 2-D with contiguous rows")
-    if t.shape[0] <= 1:
-        return cols
-    if t.stride(0) < cols:
-        raise ValueError(f"{name} has overlapping rows")
-    return t.stride(0)
+    st, shape = t.stride(), t.shape
+    if cols > 1 and st[-1] != 1:
+        raise ValueError(f"{name} must have contiguous rows")
+    ld, after = cols, 0         # `after` rows of all the dimensions so far: the next one's stride
+    for n, d in zip(shape[-2::-1], st[-2::-1]):
+        if n == 1:
+            continue
+        if after == 0:
+            ld = d
+        elif d != after:
+            raise ValueError(f"the rows of {name} must lie at one stride")
+        after = d * n
+        if ld < cols:
+            raise ValueError(f"{name} has overlapping rows")
+    return ld
 
 
 def _vector(name, t, n, dtypes=(torch.float32,)):
@@ -143,7 +155,7 @@ def embed_grad(dout, ids, vocab: int, scale: float = 1.0, dtype=None, out=None, 
     """The gradient of embed's table: row v is scale times the sum of dout's rows whose
     id is v.  Returns a vocab x dim matrix in `dtype` (default: float32), every row
     written; with `accumulate` the sums are added to `out` instead (only rows that
-    occur are touched)."""
+    occur are touched).  ids must be contiguous."""
     if stream is not None:
         return _on(stream, embed_grad, dout, ids, vocab, scale, dtype, out, accumulate)
     dev = _device("dout ids out", dout, ids, out)

@@ -237,3 +237,29 @@ def test_autograd_sees_given_outputs_change():
             call(new(*shape))
     table = new(9, 8).requires_grad_()
     assert not ops.embed(table, ids).requires_grad
+
+
+def test_rows_of_a_wider_activation():
+    """[batch, tokens, entries] views whose rows lie at one stride (a padded vocabulary's logits, a slice
+    of an activation) are matrices like any other; views whose rows do not are refused."""
+    import torch
+    from paper_2608_05088_gb300 import model_ops as ops
+    x = torch.randn(3, 7, 112, device="cuda")
+    logits, wide = x[..., :101], torch.zeros(3, 7, 104, device="cuda")
+    t, top = logits.topk(6, dim=-1)
+    loss, dx = ops.distill_loss_grad(logits.contiguous(), top, t)
+    got, dgot = ops.distill_loss_grad(logits, top[..., :6], t, dlogits=wide[..., :101])
+    assert torch.equal(got, loss) and torch.equal(dgot, dx) and not wide[..., 101:].any()
+    assert torch.equal(ops.distill_loss_grad(logits, top, t)[1], dx)
+    few = ops.distill_loss(logits.contiguous(), top[..., :2].contiguous(), t[..., :2].contiguous())
+    assert torch.equal(ops.distill_loss(logits, top[..., :2], t[..., :2])[0], few[0])
+    one = ops.distill_loss_grad(logits[1:2, 3:4], top[1:2, 3:4], t[1:2, 3:4])
+    assert torch.equal(one[1], dx[1:2, 3:4])
+    table, ids = torch.randn(50, 24, device="cuda"), torch.randint(0, 50, (3, 7), device="cuda")
+    out = torch.zeros(3, 7, 40, device="cuda")
+    assert torch.equal(ops.embed(table, ids, out=out[..., 8:32]), table[ids]) and not out[..., :8].any()
+    assert torch.equal(ops.embed_grad(out[..., 8:32], ids, 50), ops.embed_grad(table[ids], ids, 50))
+    for bad in (x[:, :-1], x[:, ::2], x[..., ::2], x.transpose(0, 1), x[:1].expand(3, 7, 112), x.transpose(1, 2)):
+        rows = torch.zeros(*bad.shape[:-1], 2, device="cuda")
+        with pytest.raises(ValueError, match="stride|contiguous|overlapping"):
+            ops.distill_loss(bad, rows.long(), rows)
