@@ -241,20 +241,27 @@ def test_autograd_sees_given_outputs_change():
 
 def test_rows_of_a_wider_activation():
     """[batch, tokens, entries] views whose rows lie at one stride (a padded vocabulary's logits, a slice
-    of an activation) are matrices like any other; views whose rows do not are refused."""
+    of an activation) are matrices like any other; views whose rows do not are refused.
+
+    A distillation sum's order goes by its row's alignment, which the views do not share with their
+    copies: two sums of 101 terms differ by twice 64 u and 8 u for each unit of depth (16 here at most),
+    a loss also by (k + 32) u of |log p| + |log q| (32 at most), a gradient by 32 u more and as much of p."""
     import torch
     from paper_2608_05088_gb300 import model_ops as ops
     x = torch.randn(3, 7, 112, device="cuda")
     logits, wide = x[..., :101], torch.zeros(3, 7, 104, device="cuda")
     t, top = logits.topk(6, dim=-1)
+    u = 2.0 ** -24
+    same_loss = lambda a, b: bool(((a - b).abs() <= 2 * u * (64 + 128 + 38 * 32)).all())
+    same_grad = lambda a, b: bool(((a - b).abs() <= 2 * u * (64 + 128 + 32 + 38)).all())
     loss, dx = ops.distill_loss_grad(logits.contiguous(), top, t)
     got, dgot = ops.distill_loss_grad(logits, top[..., :6], t, dlogits=wide[..., :101])
-    assert torch.equal(got, loss) and torch.equal(dgot, dx) and not wide[..., 101:].any()
-    assert torch.equal(ops.distill_loss_grad(logits, top, t)[1], dx)
+    assert same_loss(got, loss) and same_grad(dgot, dx) and not wide[..., 101:].any()
+    assert same_grad(ops.distill_loss_grad(logits, top, t)[1], dx)
     few = ops.distill_loss(logits.contiguous(), top[..., :2].contiguous(), t[..., :2].contiguous())
-    assert torch.equal(ops.distill_loss(logits, top[..., :2], t[..., :2])[0], few[0])
+    assert same_loss(ops.distill_loss(logits, top[..., :2], t[..., :2])[0], few[0])
     one = ops.distill_loss_grad(logits[1:2, 3:4], top[1:2, 3:4], t[1:2, 3:4])
-    assert torch.equal(one[1], dx[1:2, 3:4])
+    assert same_grad(one[1], dx[1:2, 3:4])
     table, ids = torch.randn(50, 24, device="cuda"), torch.randint(0, 50, (3, 7), device="cuda")
     out = torch.zeros(3, 7, 40, device="cuda")
     assert torch.equal(ops.embed(table, ids, out=out[..., 8:32]), table[ids]) and not out[..., :8].any()
