@@ -14,8 +14,8 @@
 // thread with a running maximum over batches of vectors; the second writes the
 // gradient and finds the row in L2.  One warp more takes the teacher's entries
 // meanwhile.  Bound by HBM: the logits once, their gradient once.  8192 rows of 50304
-// bf16 logits: 251 us, 6.26 TB/s of what has to move (loss alone 124 us, 6.7 TB/s;
-// gradient alone 254 us, 6.5 TB/s).  Rows kept in shared memory instead, by blocks that
+// bf16 logits: 251 us, 6.26 TB/s of what has to move (loss alone 123 us, 6.7 TB/s;
+// gradient alone 253 us, 6.5 TB/s).  Rows kept in shared memory instead, by blocks that
 // stay and copy the next row meanwhile, took 276 us: a block's barriers then stand
 // between its sweeps with no other block on the SM to fill them.
 //
@@ -42,7 +42,7 @@ constexpr int kMaxTop = 1024;
 // barriers (16384 rows of 8192 bf16: 105 us, wide 175; 8000 of 16384 fp32: 218, wide
 // 157).  Short and narrow: more rows at a time, for rows whose time is latency (16384 of
 // 8192 bf16: short 88 us; 6000 of 16384: short 76, medium 68; 16384 of 4000: narrow 49,
-// short 55; of 2000: narrow 34, 46 at 96 threads).
+// short 55; of 2000: narrow 35, 46 at 96 threads).
 struct Shape {
     int threads, blocks, batch;
 };

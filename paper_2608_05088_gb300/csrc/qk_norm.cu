@@ -13,7 +13,13 @@
 // neighbouring lanes, both partners of a pair in one lane, so the norm takes a
 // shuffle or two and the rotation none.  16384 tokens of 2 x 20 heads of 64 in bf16:
 // forward 31 us, 5.4 TB/s, gradient 46 us, 5.5 TB/s (a plain copy of as many bytes runs
-// at 5.6 and 5.75).  One warp per row, element by element, took 356 and 390 us.
+// at 5.6 and 5.75).
+//
+// That asks for heads and rotated parts of whole lanes, multiples of 16 entries in bf16 and
+// of 8 in fp32, on 16-byte addresses (lanes_of).  All other rows take one warp each, element
+// by element, and six to twelve times as long: 16384 tokens of 2 x 16 heads of 80 in bf16, 80
+// rotated 33 and 60 us, 40 rotated 338 and 390; heads of 64, all rotated, 25 and 39, of 72
+// 318 and 514; in fp32 72 of 72 52 and 82, 68 of 68 332 and 494.
 #include <algorithm>
 
 #include <nvtx3/nvToolsExt.h>
@@ -496,7 +502,8 @@ qk_backward_kernel(const __grid_constant__ Params P) {
 }
 
 // ------------------------------------------------------- any size and alignment
-// One warp per row, element by element.
+// One warp per row, element by element: bound by instructions (a lane loads 2 or 4 bytes at
+// a time, and a token's angles and the gains again for every head).
 template <typename T, bool INTER>
 __global__ void __launch_bounds__(kThreads)
 qk_forward_any_kernel(const __grid_constant__ Params P) {
@@ -713,7 +720,8 @@ bool vectors(const Params& P, const Rows& r) {
            (P.seq == 1 || r.seq_stride % V == 0) && r.head_stride % V == 0;
 }
 
-// Lanes of a row in the aligned kernels, 0 where they do not apply.
+// Lanes of a row in the aligned kernels, 0 where they do not apply: a lane holds two vectors
+// of 16 bytes, all turned or none.
 template <typename T, int V>
 int lanes_of(const Params& P, bool backward) {
     constexpr int N = 2 * V;
