@@ -147,9 +147,6 @@ def _prepare_head(c, g):
         m = x.amax(1)
         stats = torch.stack([m, (x - m[:, None]).exp_().sum(1)], 1)
         s["stats"] = stats * (labels >= 0)[:, None]
-        if own:     # from the forward pass whose gradient this is: its roundings cancel against the same ones
-            from paper_2608_05088_gb300 import model_ops as ops
-            s["stats"] = ops.head_loss(s["hidden"], s["table"], s["labels"], weight=s["weight"])[1]
         s["dloss"] = 1.0 + 0.1 * torch.randn(n, generator=g, device=DEV)
     if c["accumulate"]:
         s["dtable"] = _normal(g, (v, d), c["table"], 1e-3)
