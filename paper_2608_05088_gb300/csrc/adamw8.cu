@@ -183,7 +183,7 @@ __device__ __forceinline__ uint32_t m_code(float m, float inverse, uint32_t rand
     return code == 0 ? 0u : code | (__float_as_uint(m) >> 24 & 0x80u);
 }
 __device__ __forceinline__ uint32_t root_code(float root, float inverse, uint32_t random) {
-    const uint32_t code = (__float_as_uint(root * inverse * kDown) + (random << 2)) >> 18;
+    const uint32_t code = (__float_as_uint(fabsf(root) * inverse * kDown) + (random << 2)) >> 18;     // (-0: 0)
     return code == 0 && root > 0.f ? 1u : code;
 }
 
