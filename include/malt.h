@@ -480,7 +480,9 @@ void malt_adamw8_destroy_state(malt_adamw8_state_t* st);
  * s = sqrt(v) of tensor after tensor, each starting at a multiple of 256
  * elements, in two device buffers of dtype MALT_F32 or MALT_BF16 (both exact).
  * get writes zeros behind a tensor's elements; set rounds to the nearest code
- * (a negative s makes both NaN).  Enqueued on `stream`. */
+ * (a negative s makes both NaN, -0 is 0).  Enqueued on `stream`, one of them at a
+ * time; get changes nothing that a step reads, and one that runs beside a step
+ * takes old or new codes.  get_step waits for the last step's stream alone. */
 int malt_adamw8_get_moments(malt_adamw8_state_t* st, const malt_adamw8_param_t* params, int32_t n, void* m, void* root,
                             int32_t dtype, void* stream);
 int malt_adamw8_set_moments(malt_adamw8_state_t* st, const malt_adamw8_param_t* params, int32_t n, const void* m,

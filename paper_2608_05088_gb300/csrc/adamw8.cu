@@ -661,11 +661,12 @@ struct malt_adamw8_state {
     std::vector<malt_adamw8_param_t> shape0;    // sizes and gradient types fixed at init
     void* ws = nullptr;
     Desc* d_desc = nullptr;
-    Ptrs* d_ptrs = nullptr;
+    Ptrs* d_ptrs = nullptr;         // of steps
+    Ptrs* d_moment_ptrs = nullptr;  // of read-outs and sets: they may run beside a step's two launches
     Clock* d_clock = nullptr;
     Start* d_starts = nullptr;
     int32_t grid = 0;
-    cudaStream_t last_stream = nullptr;
+    cudaStream_t last_stream = nullptr, moments_stream = nullptr;
 };
 
 namespace {
@@ -683,7 +684,7 @@ int check_same(const malt_adamw8_state* st, const malt_adamw8_param_t* params, i
     return MALT_OK;
 }
 
-// hp: of a step, which the device's clock counts; null for none.
+// hp: of a step, which the device's clock counts; null for the moments' table.
 template <int N>
 cudaError_t bind_some(const malt_adamw8_state* st, const malt_adamw8_param_t* params, int off, int count,
                       const malt_adamw_hparams_t* hp, cudaStream_t s) {
@@ -699,10 +700,10 @@ cudaError_t bind_some(const malt_adamw8_state* st, const malt_adamw8_param_t* pa
         B.p[i] = Ptrs{p.w, p.w_copy, p.g, p.m, p.m_scale, p.v, p.v_scale, decay, 0};
     }
     for (int i = count; i < N; ++i) B.p[i] = Ptrs{};
-    return malt::launch_chained(bind_kernel<N>, 1, N, 0, s, B, st->d_ptrs);
+    return malt::launch_chained(bind_kernel<N>, 1, N, 0, s, B, hp != nullptr ? st->d_ptrs : st->d_moment_ptrs);
 }
 int bind(malt_adamw8_state* st, const malt_adamw8_param_t* params, const malt_adamw_hparams_t* hp, cudaStream_t s) {
-    st->last_stream = s;
+    (hp != nullptr ? st->last_stream : st->moments_stream) = s;
     ADAMW8_CUDA(cudaSetDevice(st->device), "cudaSetDevice");
     for (int off = 0; off == 0 || off < st->n; off += kBindChunk) {
         const int count = std::min(kBindChunk, st->n - off);
@@ -728,8 +729,9 @@ int moments(malt_adamw8_state* st, const malt_adamw8_param_t* params, int32_t n,
     rc = bind(st, params, nullptr, s);
     if (rc == MALT_OK) {
         const cudaError_t e =
-            dtype == MALT_BF16 ? launch_moments<GET, bf16>(st->d_desc, st->d_ptrs, n, kRuns * st->grid, st->d_starts, m, root, s)
-                               : launch_moments<GET, float>(st->d_desc, st->d_ptrs, n, kRuns * st->grid, st->d_starts, m, root, s);
+            dtype == MALT_BF16
+                ? launch_moments<GET, bf16>(st->d_desc, st->d_moment_ptrs, n, kRuns * st->grid, st->d_starts, m, root, s)
+                : launch_moments<GET, float>(st->d_desc, st->d_moment_ptrs, n, kRuns * st->grid, st->d_starts, m, root, s);
         rc = malt::cuda_status(e, name);
     }
     nvtxRangePop();
@@ -789,7 +791,8 @@ int malt_adamw8_init_state(malt_adamw8_state_t** out, const malt_adamw8_param_t*
         }
         const size_t nn = static_cast<size_t>(std::max(n, 1));
         auto aligned = [](size_t x) { return (x + 255) & ~size_t(255); };
-        const size_t o_ptrs = aligned(sizeof(Desc) * nn), o_clock = aligned(o_ptrs + sizeof(Ptrs) * nn);
+        const size_t o_ptrs = aligned(sizeof(Desc) * nn), o_moment_ptrs = aligned(o_ptrs + sizeof(Ptrs) * nn);
+        const size_t o_clock = aligned(o_moment_ptrs + sizeof(Ptrs) * nn);
         const size_t o_starts = o_clock + 256, bytes = aligned(o_starts + sizeof(Start) * (kRuns * st->grid + 1));
         if (cudaMalloc(&st->ws, bytes) != cudaSuccess) {
             st->ws = nullptr;
@@ -799,6 +802,7 @@ int malt_adamw8_init_state(malt_adamw8_state_t** out, const malt_adamw8_param_t*
         uint8_t* const base = static_cast<uint8_t*>(st->ws);
         st->d_desc = reinterpret_cast<Desc*>(base);
         st->d_ptrs = reinterpret_cast<Ptrs*>(base + o_ptrs);
+        st->d_moment_ptrs = reinterpret_cast<Ptrs*>(base + o_moment_ptrs);
         st->d_clock = reinterpret_cast<Clock*>(base + o_clock);
         st->d_starts = reinterpret_cast<Start*>(base + o_starts);
         cudaStream_t s = static_cast<cudaStream_t>(stream);
@@ -821,7 +825,7 @@ int malt_adamw8_init_state(malt_adamw8_state_t** out, const malt_adamw8_param_t*
         // (streams that do not wait for the default one may step next)
         if (rc == MALT_OK) rc = malt::cuda_status(cudaStreamSynchronize(nullptr), "cudaStreamSynchronize");
         if (rc != MALT_OK) return fail(rc);
-        st->last_stream = s;
+        st->last_stream = st->moments_stream = s;
     } catch (...) {         // no host memory: no exception leaves a C entry
         delete st;
         return MALT_ERR_OUT_OF_MEMORY;
@@ -881,6 +885,7 @@ int malt_adamw8_set_step(malt_adamw8_state_t* st, int64_t t_host) {
 void malt_adamw8_destroy_state(malt_adamw8_state_t* st) {
     if (st == nullptr) return;
     cudaStreamSynchronize(st->last_stream);
+    cudaStreamSynchronize(st->moments_stream);
     if (st->ws != nullptr) cudaFree(st->ws);
     delete st;
 }

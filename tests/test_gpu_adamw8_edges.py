@@ -28,3 +28,28 @@ def test_roots_of_negative_zero():
         assert all((x == y).all() for x, y in zip(ref.values(*got), ref.values(*want)))
     assert intact()
     opt.close()
+
+
+def test_reading_moments_beside_steps():
+    """A read-out on another stream changes nothing of a step, and the count waits for the steps."""
+    import torch
+    malt, params, _ = make([300_000] * 8 + [7] * 30, torch.bfloat16)
+    twin = make([300_000] * 8 + [7] * 30, torch.bfloat16)[1]
+    read, alone = malt.AdamW8(params, seed=1), malt.AdamW8(twin, seed=1)
+    hp = malt.adamw_hparams(lr=1e-2)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    torch.cuda._sleep(100_000_000)              # cycles: the steps below wait for it, the read-outs do not
+    read.step(hp)
+    read.moments(stream=side)
+    assert read.get_step() == 1
+    alone.step(hp)
+    for _ in range(300):
+        read.step(hp)
+        read.moments(dtype=torch.bfloat16, stream=side)
+        alone.step(hp)
+    torch.cuda.synchronize()
+    for p, q in zip(params, twin):
+        assert all(torch.equal(x, y) for x, y in zip(p[:7], q[:7]) if x is not None)
+    read.close()
+    alone.close()
