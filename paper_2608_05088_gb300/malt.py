@@ -775,15 +775,17 @@ class AdamW8:
     m_scale, v, v_scale, weight_decay) device tensors; the states (adamw8_states makes them) are zeroed at
     construction.  seed: of the states' random rounding.
 
-    The tensors are checked and their addresses taken once, here: their memory is kept, and steps go on
-    with it until `params` gives others (checks of hundreds of tensors take the host longer than the GPU
-    their update)."""
+    The tensors are checked in full here, and again where one of them has moved (its `.data` was replaced, its
+    storage resized): checks of hundreds of tensors take the host longer than the GPU their update, a look at
+    their addresses half of it."""
 
     def __init__(self, params, seed: int = 0, stream=None):
         import torch
-        self.params = tuple(params)
-        self._memory = [t.untyped_storage() for p in self.params for t in p if isinstance(t, torch.Tensor)]
+        self.params = tuple(map(tuple, params))
+        self._tensors = [t for p in self.params for t in p if isinstance(t, torch.Tensor)]
+        self._codes = [t for p in self.params for t in p[3:7]]
         self._array = adamw8_params_array(self.params)
+        self._at, self._codes_at = self._addresses(self._tensors), self._addresses(self._codes)
         if any(p[0].get_device() < 0 for p in self.params):
             raise ValueError("the tensors must be on a CUDA device")
         self._elements = sum(-(-p[0].numel() // ADAMW8_BLOCK) for p in self.params) * ADAMW8_BLOCK
@@ -791,9 +793,33 @@ class AdamW8:
         self._on = torch.device("cuda", self._device)
         self.state = malt_adamw8_init_state(self.params, seed, stream)
 
+    @staticmethod
+    def _addresses(tensors):
+        import torch
+        return list(map(torch.Tensor.data_ptr, tensors))
+
+    def _moved(self):
+        """The tensors checked again, where they lie now."""
+        for t in self._tensors:
+            if t.untyped_storage().nbytes() < (t.storage_offset() + t.numel()) * t.element_size():
+                raise ValueError("a tensor's storage has been resized to less than the tensor")
+        self._array = adamw8_params_array(self.params)
+        self._at, self._codes_at = self._addresses(self._tensors), self._addresses(self._codes)
+
     def step(self, hp: malt_adamw_hparams_t, stream=None, params=None):
-        arr, n = (self._array, len(self.params)) if params is None else (adamw8_params_array(params), len(params))
+        """params: other tensors for this step."""
+        if params is not None:
+            arr, n = adamw8_params_array(params), len(params)
+        else:
+            if self._addresses(self._tensors) != self._at:
+                self._moved()
+            arr, n = self._array, len(self.params)
         _check(load().malt_adamw8_step(self.state, arr, n, ctypes.byref(hp), self._stream(stream)), "malt_adamw8_step")
+
+    def _codes_array(self):
+        if self._addresses(self._codes) != self._codes_at:
+            self._moved()
+        return self._array
 
     def _stream(self, stream):
         """The raw handle of a stream, by default the current one of the tensors' device."""
@@ -821,16 +847,16 @@ class AdamW8:
                 t.record_stream(caller)
             return out
         dtype = dtype or torch.float32
-        code = _dtype_code_of(dtype)
+        code, arr = _dtype_code_of(dtype), self._codes_array()
         m = torch.empty(self._elements, dtype=dtype, device=self._on)
         root = torch.empty_like(m)
-        _check(load().malt_adamw8_get_moments(self.state, self._array, len(self.params), m.data_ptr(), root.data_ptr(), code,
+        _check(load().malt_adamw8_get_moments(self.state, arr, len(self.params), m.data_ptr(), root.data_ptr(), code,
                                               self._stream(None)), "malt_adamw8_get_moments")
         return m, root
 
     def set_moments(self, m, root, stream=None):
         """States of these values, laid out as moments returns them, rounded to the nearest code."""
-        _adamw8_moments("malt_adamw8_set_moments", self.state, self.params, self._array, m, root, stream)
+        _adamw8_moments("malt_adamw8_set_moments", self.state, self.params, self._codes_array(), m, root, stream)
 
     def get_step(self) -> int:
         return malt_adamw8_get_step(self.state)
