@@ -541,12 +541,26 @@ def adamw8_params_array(params):
     return (malt_adamw8_param_t * len(n)).from_buffer(words)
 
 
+def _adamw8_device(params) -> int:
+    """The current CUDA device, which the tensors are on: a state belongs to it."""
+    import torch
+    dev = torch.cuda.current_device() if not params or params[0][0].get_device() >= 0 else -1
+    if dev < 0 or (params and params[0][0].get_device() != dev):
+        raise ValueError(f"the tensors must be on the current CUDA device, not {params[0][0].device}")
+    return dev
+
+
 def malt_adamw8_init_state(params, seed: int = 0, stream=None) -> ctypes.c_void_p:
+    return _adamw8_init(params, adamw8_params_array(params), seed, stream)
+
+
+def _adamw8_init(params, arr, seed, stream):
     st = ctypes.c_void_p()
     if not 0 <= seed < 1 << 32:
         raise ValueError("seed must be a 32-bit unsigned integer")
-    _check(load().malt_adamw8_init_state(ctypes.byref(st), adamw8_params_array(params), len(params), seed,
-                                         _stream_handle(stream)), "malt_adamw8_init_state")
+    _adamw8_device(params)
+    _check(load().malt_adamw8_init_state(ctypes.byref(st), arr, len(params), seed, _stream_handle(stream)),
+           "malt_adamw8_init_state")
     return st
 
 
@@ -555,7 +569,7 @@ def malt_adamw8_step(st, params, hp: malt_adamw_hparams_t, stream=None):
                                    _stream_handle(stream)), "malt_adamw8_step")
 
 
-def _adamw8_moments(name, st, params, arr, m, root, stream):
+def _adamw8_moments(name, st, params, arr, m, root, handle):
     import torch
     total = sum(-(-p[0].numel() // ADAMW8_BLOCK) for p in params) * ADAMW8_BLOCK
     for t in (m, root):
@@ -566,15 +580,15 @@ def _adamw8_moments(name, st, params, arr, m, root, stream):
         if params and t.device != params[0][0].device:
             raise ValueError("moments must be on the device of the tensors")
     _check(getattr(load(), name)(st, adamw8_params_array(params) if arr is None else arr, len(params), m.data_ptr(),
-                                 root.data_ptr(), _dtype_code(m), _stream_handle(stream)), name)
+                                 root.data_ptr(), _dtype_code(m), handle), name)
 
 
 def malt_adamw8_get_moments(st, params, m, root, stream=None):
-    _adamw8_moments("malt_adamw8_get_moments", st, params, None, m, root, stream)
+    _adamw8_moments("malt_adamw8_get_moments", st, params, None, m, root, _stream_handle(stream))
 
 
 def malt_adamw8_set_moments(st, params, m, root, stream=None):
-    _adamw8_moments("malt_adamw8_set_moments", st, params, None, m, root, stream)
+    _adamw8_moments("malt_adamw8_set_moments", st, params, None, m, root, _stream_handle(stream))
 
 
 def malt_adamw8_get_step(st) -> int:
@@ -786,12 +800,10 @@ class AdamW8:
         self._codes = [t for p in self.params for t in p[3:7]]
         self._array = adamw8_params_array(self.params)
         self._at, self._codes_at = self._addresses(self._tensors), self._addresses(self._codes)
-        if any(p[0].get_device() < 0 for p in self.params):
-            raise ValueError("the tensors must be on a CUDA device")
         self._elements = sum(-(-p[0].numel() // ADAMW8_BLOCK) for p in self.params) * ADAMW8_BLOCK
-        self._device = self.params[0][0].get_device() if self.params else torch.cuda.current_device()
+        self._device = _adamw8_device(self.params)
         self._on = torch.device("cuda", self._device)
-        self.state = malt_adamw8_init_state(self.params, seed, stream)
+        self.state = _adamw8_init(self.params, self._array, seed, stream)
 
     @staticmethod
     def _addresses(tensors):
@@ -803,13 +815,20 @@ class AdamW8:
         for t in self._tensors:
             if t.untyped_storage().nbytes() < (t.storage_offset() + t.numel()) * t.element_size():
                 raise ValueError("a tensor's storage has been resized to less than the tensor")
-        self._array = adamw8_params_array(self.params)
+        self._array = self._checked(self.params)
         self._at, self._codes_at = self._addresses(self._tensors), self._addresses(self._codes)
+
+    def _checked(self, params):
+        """The array of tensors on the state's device."""
+        arr = adamw8_params_array(params)
+        if len(params) and params[0][0].get_device() != self._device:
+            raise ValueError(f"the tensors must be on {self._on}, where the state is, not on {params[0][0].device}")
+        return arr
 
     def step(self, hp: malt_adamw_hparams_t, stream=None, params=None):
         """params: other tensors for this step."""
         if params is not None:
-            arr, n = adamw8_params_array(params), len(params)
+            arr, n = self._checked(params), len(params)
         else:
             if self._addresses(self._tensors) != self._at:
                 self._moved()
@@ -840,7 +859,7 @@ class AdamW8:
         tensor each (spans says where), zeros between them."""
         import torch
         if stream is not None:
-            caller = torch.cuda.current_stream()
+            caller = torch.cuda.current_stream(self._on)
             with torch.cuda.stream(stream):
                 out = self.moments(dtype)
             for t in out:
@@ -856,7 +875,8 @@ class AdamW8:
 
     def set_moments(self, m, root, stream=None):
         """States of these values, laid out as moments returns them, rounded to the nearest code."""
-        _adamw8_moments("malt_adamw8_set_moments", self.state, self.params, self._codes_array(), m, root, stream)
+        _adamw8_moments("malt_adamw8_set_moments", self.state, self.params, self._codes_array(), m, root,
+                        self._stream(stream))
 
     def get_step(self) -> int:
         return malt_adamw8_get_step(self.state)
