@@ -8,6 +8,7 @@ library has not been built (there is no fallback of any kind).
 from __future__ import annotations
 
 import array
+import bisect
 import ctypes
 import itertools
 import operator
@@ -532,8 +533,18 @@ def adamw8_params_array(params):
     g_dt = [codes[d] if d in codes else _dtype_code(t) for t, d in zip(g, map(dtype_of, g))]
     if len(set(map(T.get_device, itertools.chain(w, g, m, ms, v, vs, copies)))) != 1:
         raise ValueError("all tensors must be on one device")
-    if len(set(map(T.data_ptr, itertools.chain(w, m, ms, v, vs, copies)))) != 5 * len(n) + len(copies):
+    # (contiguous, and of known sizes: w takes 4 bytes an element, codes and scales one, a copy two)
+    start = list(map(T.data_ptr, itertools.chain(w, m, v, ms, vs, copies)))
+    size = [4 * k for k in n] + n + n + blocks + blocks + [2 * c.numel() for c in copies]
+    written = sorted(zip(start, size))
+    ends = [a + k for a, k in written]
+    starts = [a for a, _ in written]
+    if any(map(operator.gt, ends, starts[1:])) or len(set(starts)) != len(starts):
         raise ValueError("no two of the tensors that are written may share memory")
+    for t, k in zip(map(T.data_ptr, g), (d.itemsize * k for d, k in zip(map(dtype_of, g), n))):
+        i = bisect.bisect_left(starts, t + k)       # the last that starts before its end
+        if i > 0 and ends[i - 1] > t:
+            raise ValueError("gradients may not share memory with a tensor that is written")
     # Every field starts on an 8-byte boundary: ten 64-bit words.
     rows = zip(map(T.data_ptr, w), [0 if c is None else c.data_ptr() for c in wc], map(T.data_ptr, g), g_dt,
                map(T.data_ptr, m), map(T.data_ptr, ms), map(T.data_ptr, v), map(T.data_ptr, vs), n, _float_words(wd))
