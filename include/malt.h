@@ -695,7 +695,8 @@ int malt_distill_forward_backward(const malt_distill_t* d, float* loss, float* s
  * of multiples of 8, in bf16 parts.  malt_head_workspace_bytes gives its size for
  * the calls (forward, gradient: which of them) on these sizes, types and
  * alignments, 0 for what the calls refuse.  Workspaces are 256-byte aligned.
- * Outputs may not lie in the inputs' memory or in one another's.  Should a wait
+ * Outputs and workspace may not lie in the inputs' memory or in one another's
+ * (columns of one matrix apart do not).  Should a wait
  * inside a kernel run out (a second and more: nothing here waits that long), all
  * losses and dhidden are NaN, and dtable is not to be used.
  * rows <= 2^22, dim <= 2^16, vocab <= 2^24, and fewer than 2^30 tiles of 256. */

@@ -1893,14 +1893,27 @@ int run(const malt_head_t* h, const Outputs& O, bool forward, bool gradient, voi
         if (!aligned_to(O.dtable, type_bytes(O.dtable_dtype)) || !aligned_to(O.dhidden, type_bytes(h->hidden_dtype)))
             return MALT_ERR_MISALIGNED;
     }
-    if (workspace == nullptr || bytes < static_cast<size_t>(layout_of(h, forward, gradient).bytes)) return MALT_ERR_INVALID_ARG;
+    const int64_t need = layout_of(h, forward, gradient).bytes;
+    if (workspace == nullptr || bytes < static_cast<size_t>(need)) return MALT_ERR_INVALID_ARG;
     if (!aligned_to(workspace, 256)) return MALT_ERR_MISALIGNED;
     if (h->rows == 0 && !gradient) return MALT_OK;
     if (h->rows == 0 && O.accumulate) return MALT_OK;
-    // (the table and the hidden rows are read while gradients are written)
-    if (gradient && (O.dtable == h->table || O.dtable == h->hidden || (h->rows > 0 && (O.dhidden == h->table ||
-                     O.dhidden == h->hidden || O.dhidden == O.dtable))))
-        return MALT_ERR_INVALID_ARG;
+    // (inputs are read while outputs are written)
+    const int hidden_bytes = type_bytes(h->hidden_dtype);
+    const Extent out[] = {extent_of(O.loss, 4 * h->rows), extent_of(O.stats, 8 * h->rows),
+                          extent_of(O.dhidden, h->rows, h->dim, O.dhidden_ld, hidden_bytes),
+                          extent_of(O.dtable, h->vocab, h->dim, O.dtable_ld, type_bytes(O.dtable_dtype)),
+                          extent_of(workspace, need)};
+    const Extent in[] = {extent_of(h->hidden, h->rows, h->dim, h->hidden_ld, hidden_bytes),
+                         extent_of(h->table, h->vocab, h->dim, h->table_ld, type_bytes(h->table_dtype)),
+                         extent_of(h->labels, type_bytes(h->labels_dtype) * h->rows), extent_of(h->weight, 4 * h->rows),
+                         extent_of(O.in_stats, 8 * h->rows), extent_of(O.dloss, 4 * h->rows)};
+    for (const Extent& o : out) {
+        for (const Extent& i : in)
+            if (overlap(o, i)) return MALT_ERR_INVALID_ARG;
+        for (const Extent* other = out; other != &o; ++other)
+            if (overlap(o, *other)) return MALT_ERR_INVALID_ARG;
+    }
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     if (h->rows == 0)
         return cuda_status(cudaMemset2DAsync(O.dtable, O.dtable_ld * type_bytes(O.dtable_dtype), 0,

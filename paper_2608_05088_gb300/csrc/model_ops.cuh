@@ -11,6 +11,7 @@
 
 #include "../../include/malt.h"
 #include "chain.cuh"
+#include "extent.h"
 
 namespace malt {
 
