@@ -606,7 +606,8 @@ int malt_qk_norm_backward(const malt_qk_norm_t* p, const malt_heads_t* dq_out, c
  * rows, whose workspace is malt_rms_norm_workspace_bytes (0 for sizes that the
  * call refuses; without dgain none is needed).
  * h and y may each be x's or the residual's buffer (not both the same), dx dy's,
- * h's or dh's, with the same leading dimension and type.  dim and leading dimensions
+ * h's or dh's, with the same leading dimension and type; else what is written may
+ * not lie in another operand's memory.  dim and leading dimensions
  * that are multiples of 8 on 16-byte addresses (codes 8) run faster.  dim <= 2^24,
  * tokens < 2^31 - 64. */
 typedef struct {

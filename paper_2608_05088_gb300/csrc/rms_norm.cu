@@ -15,6 +15,7 @@
 #include <cuda_fp8.h>
 
 #include <algorithm>
+#include <initializer_list>
 
 #include <nvtx3/nvToolsExt.h>
 
@@ -489,11 +490,23 @@ int check_rows(const malt_rows_t* r, const malt_rms_norm_t* p, bool bytes = fals
     return bytes || aligned_to(r->data, type_bytes(r->dtype)) ? MALT_OK : MALT_ERR_MISALIGNED;
 }
 
-// Whether an output may lie where an input does: elsewhere, or entry on entry.
-bool may_share(const malt_rows_t* out, const malt_rows_t* in) {
-    return out == nullptr || in == nullptr || out->data == nullptr || out->data != in->data ||
-           (out->ld == in->ld && out->dtype == in->dtype);
+Extent place_of(const malt_rows_t* r, const malt_rms_norm_t* p) {
+    if (r == nullptr) return {};
+    return extent_of(r->data, p->tokens, p->dim, r->ld, r->dtype == MALT_E4M3 ? 1 : type_bytes(r->dtype));
 }
+// Whether an output may lie where an input does: elsewhere, or entry on entry.
+bool may_share(const malt_rows_t* out, const malt_rows_t* in, const malt_rms_norm_t* p) {
+    if (out == nullptr || in == nullptr) return true;
+    if (out->data == in->data && out->ld == in->ld && out->dtype == in->dtype) return true;
+    return !overlap(place_of(out, p), place_of(in, p));
+}
+// Whether what is written beside them lies apart from all of them.
+bool apart(const Extent& e, std::initializer_list<const malt_rows_t*> rows, const malt_rms_norm_t* p) {
+    for (const malt_rows_t* r : rows)
+        if (overlap(e, place_of(r, p))) return false;
+    return true;
+}
+Extent gain_extent(const malt_rms_norm_t* p) { return extent_of(p->gain, p->dim * type_bytes(p->gain_dtype)); }
 
 int check(const malt_rms_norm_t* p) {
     if (p == nullptr || p->tokens < 0 || p->dim < 1 || !(p->eps >= 0.f)) return MALT_ERR_INVALID_ARG;
@@ -590,8 +603,11 @@ int forward(const malt_rms_norm_t* p, const malt_rows_t* x, const malt_rows_t* r
     if (rc == MALT_OK) rc = check_rows(y, p, scales != nullptr);
     if (rc != MALT_OK) return rc;
     if (p->tokens == 0) return MALT_OK;
-    if (!may_share(h, x) || !may_share(h, residual) || !may_share(y, x) || !may_share(y, residual) ||
-        (h != nullptr && h->data == y->data))
+    const Extent gain = gain_extent(p);
+    const Extent of_scales = extent_of(scales, p->tokens, (p->dim + kGroup - 1) / kGroup, scales_ld, 4);
+    if (!may_share(h, x, p) || !may_share(h, residual, p) || !may_share(y, x, p) || !may_share(y, residual, p) ||
+        !apart(place_of(y, p), {h}, p) || !apart(gain, {h, y}, p) || !apart(of_scales, {x, residual, h, y}, p) ||
+        overlap(of_scales, gain))
         return MALT_ERR_INVALID_ARG;
     Params P = params_of(p);
     P.x = rows_of(x), P.s = rows_of(residual), P.h = rows_of(h), P.y = rows_of(y);
@@ -689,13 +705,19 @@ int malt_rms_norm_backward(const malt_rms_norm_t* p, const malt_rows_t* dy, cons
     if (rc == MALT_OK) rc = check_rows(dx, p);
     if (rc != MALT_OK) return rc;
     if (dx->dtype != h->dtype || (dh != nullptr && dh->dtype != h->dtype)) return MALT_ERR_UNSUPPORTED;
-    if (!may_share(dx, dy) || !may_share(dx, h) || !may_share(dx, dh)) return MALT_ERR_INVALID_ARG;
+    if (!may_share(dx, dy, p) || !may_share(dx, h, p) || !may_share(dx, dh, p)) return MALT_ERR_INVALID_ARG;
     if (!aligned_to(dgain, 4)) return MALT_ERR_MISALIGNED;
     if (dgain != nullptr) {
         if (workspace == nullptr || workspace_bytes < malt_rms_norm_workspace_bytes(p->tokens, p->dim))
             return MALT_ERR_INVALID_ARG;
         if (!aligned_to(workspace, 16)) return MALT_ERR_MISALIGNED;
     }
+    const Extent gain = gain_extent(p), of_gain = extent_of(dgain, p->dim * 4);
+    const Extent parts =
+        extent_of(dgain != nullptr ? workspace : nullptr, static_cast<int64_t>(malt_rms_norm_workspace_bytes(p->tokens, p->dim)));
+    if (!apart(gain, {dx}, p) || !apart(of_gain, {dy, h, dh, dx}, p) || !apart(parts, {dy, h, dh, dx}, p) ||
+        overlap(gain, of_gain) || overlap(gain, parts) || overlap(of_gain, parts))
+        return MALT_ERR_INVALID_ARG;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     if (p->tokens == 0) {
         if (dgain == nullptr) return MALT_OK;

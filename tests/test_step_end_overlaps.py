@@ -7,7 +7,7 @@ import pytest
 import torch
 
 from paper_2608_05088_gb300 import build, malt
-from tests.test_step_end_refusals import BAD, BF16, head
+from tests.test_step_end_refusals import BAD, BF16, F32, head, rms, rows
 
 A = 1 << 20         # addresses that nothing reads: every call here fails before a launch
 M = 1 << 16
@@ -57,6 +57,40 @@ def test_head_in_one_matrix(lib, first):
     """dhidden among hidden's rows of 64, 160 apart, over some of their entries."""
     assert call_head(lib, h_ld=160, dh_ld=160, dhidden=PLACES["hidden"] + 2 * first) == BAD
     assert call_head(lib, h_ld=160, dh_ld=200, dhidden=PLACES["hidden"] + 2 * 64) == BAD
+
+
+# 4 rows of 16 fp32 entries: 256 bytes; a gain of 64, scales of 16
+X, S, H, Y, G, C, DG, WS = (A + k * M for k in range(8))
+
+
+def test_norm(lib):
+    """Offsets into an input, and outputs in one another, in the gain and in the scales."""
+    def forward(x=X, s=S, h=H, y=Y, gain=G, scales=None, ld=16):
+        p, r = rms(gain=gain), lambda at, dtype=F32: rows(data=at, ld=ld, dtype=dtype)
+        add = (None, None) if s is None else (r(s), r(h))
+        if scales is None:
+            return lib.malt_rms_norm_forward(p, r(x), *add, r(y), None)
+        return lib.malt_rms_norm_forward_8bit(p, r(x), *add, r(y, malt.MALT_E4M3), scales, 1, None)
+
+    for bad in (dict(y=X + 64), dict(y=X - 64), dict(y=S + 192), dict(h=X + 16), dict(h=S - 240), dict(h=Y), dict(h=Y + 64),
+                dict(y=G), dict(h=G - 240), dict(y=X + 4, s=None), dict(x=X, s=X + 64, h=X), dict(y=X + 32, ld=20),
+                dict(x=X, y=X + 40, ld=24, s=None)):
+        assert forward(**bad) == BAD, bad
+    for bad in (dict(scales=X), dict(scales=S + 252), dict(scales=H - 12), dict(scales=Y + 60), dict(scales=G + 60),
+                dict(scales=C, y=X + 255), dict(scales=C, y=C), dict(scales=C, h=C)):
+        assert forward(**bad) == BAD, bad
+
+
+def test_norm_gradient(lib):
+    need = lib.malt_rms_norm_workspace_bytes(4, 16)
+
+    def backward(dy=X, h=H, dh=S, dx=Y, gain=G, dgain=DG, ws=WS):
+        r = lambda at: rows(data=at)
+        return lib.malt_rms_norm_backward(rms(gain=gain), r(dy), r(h), r(dh), r(dx), dgain, ws, need, None)
+
+    for bad in (dict(dx=X + 64), dict(dx=H - 240), dict(dx=S + 4), dict(dx=G), dict(dgain=X), dict(dgain=H + 252), dict(dgain=S - 60),
+                dict(dgain=Y), dict(dgain=G + 60), dict(dgain=WS + need - 4), dict(ws=X), dict(ws=Y + 240), dict(ws=G - need + 16)):
+        assert backward(**bad) == BAD, bad
 
 
 SOURCE = r"""
