@@ -44,6 +44,14 @@ def test_reading_moments_beside_steps():
     read.moments(stream=side)
     assert read.get_step() == 1
     alone.step(hp)
+    steps = torch.cuda.Stream()
+    steps.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(steps):              # (a stream that the default one does not wait for)
+        torch.cuda._sleep(100_000_000)
+        read.step(hp)
+    read.moments(stream=side)
+    assert read.get_step() == 2
+    alone.step(hp)
     for _ in range(300):
         read.step(hp)
         read.moments(dtype=torch.bfloat16, stream=side)

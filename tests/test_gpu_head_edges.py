@@ -1,9 +1,9 @@
-"""The output head at its edges: operands in one matrix."""
-import numpy as np
+"""The output head at its edges: operands in one matrix, sums in parts, views of a table whose rows are no whole
+16 bytes."""
 import pytest
 
 from tests.test_gpu_head import BF16, case
-from tests.test_gpu_model_ops import torch_and_ops
+from tests.test_gpu_model_ops import placed, torch_and_ops
 
 pytestmark = pytest.mark.gpu
 
@@ -24,3 +24,51 @@ def test_columns_of_one_matrix():
         args = (X, W) if bad.get("dhidden") is X or bad.get("dtable") is W else (both[:, :64], tables[:, 64:128])
         with pytest.raises(ops.malt.MaltError):
             ops.head_loss_grad(*args, Y, weight=C, **bad)
+
+
+# What fills several parts: logits of more than 2048 entries (turned, and not); dtable of more than 1024 rows that
+# count, as boxes and element by element; dhidden of pieces of more than 1024 entries.
+@pytest.mark.parametrize("rows,dim,vocab", [(24, 2200, 300), (300, 2200, 600), (1500, 132, 700), (1500, 101, 700),
+                                            (1531, 501, 32003)])
+@pytest.mark.parametrize("accumulate", [False, True])
+def test_fp32_sums_in_parts(rows, dim, vocab, accumulate):
+    """Against fp64 products.  A sum's parts lose what a sum of 32 or 16 slices of 64 does, so that relative 2-norms stay
+    where those of one part are: with random signs some 1e-6; a part lost or taken twice is off by its share."""
+    torch, ops = torch_and_ops()
+    g = torch.Generator(device="cuda").manual_seed(rows + dim)
+    W = torch.randn(vocab, dim, generator=g, device="cuda") * 1.5 / dim ** 0.5
+    Y = torch.randint(0, vocab, (rows,), generator=g, device="cuda")
+    X = torch.randn(rows, dim, generator=g, device="cuda") + 2 * W[Y]
+    Y[torch.rand(rows, generator=g, device="cuda") < 0.1] = -1
+    old = torch.randn(vocab, dim, generator=g, device="cuda") * 0.1
+    dtable = old.clone() if accumulate else None
+    loss, dh, dw = ops.head_loss_grad(X, W, Y, dtable=dtable, accumulate=accumulate)
+    _, stats = ops.head_loss(X, W, Y)
+    on = Y >= 0
+    x, w = X.double()[on], W.double()
+    l = x @ w.t()
+    m = l.max(1).values
+    lse = torch.logsumexp(l, 1)
+    at = torch.arange(len(x), device="cuda")
+    p = torch.exp(l - lse[:, None])
+    p[at, Y[on]] -= 1
+    near = lambda a, b, tol: float((a.double() - b).norm() / b.norm()) < tol
+    assert near(loss[on], lse - l[at, Y[on]], 1e-5) and near(stats[on, 0], m, 3e-6)
+    assert near(stats[on, 1], (lse - m).exp(), 1e-5)
+    assert near(dh[on], p @ w, 5e-6) and float(dh[~on].abs().sum()) == 0
+    want = p.t() @ x
+    assert near(dw.double() - old if accumulate else dw, want, 5e-6)
+
+
+def test_views_of_a_table_with_odd_rows():
+    """Rows whose last 16 bytes are shared with what lies behind them: it is not read into the logits."""
+    torch, ops = torch_and_ops()
+    for rows in (40, 300):
+        for dim, ld in ((21, 24), (45, 48), (61, 72), (129, 136)):
+            hidden, table, labels, weight = case(rows, dim, 700, BF16, BF16, seed=dim)
+            X, Y, C = torch.as_tensor(hidden).bfloat16().cuda(), torch.as_tensor(labels).cuda(), torch.as_tensor(weight).cuda()
+            W = placed(table, torch.bfloat16, ld)         # NaN behind every row
+            want = ops.head_loss_grad(X, W.contiguous(), Y, weight=C)
+            got = ops.head_loss_grad(X, W, Y, weight=C)
+            assert all(bool(t.isfinite().all()) for t in got)
+            assert all(torch.equal(a, b) for a, b in zip(got, want))
