@@ -63,12 +63,18 @@ constexpr int32_t kEnd = -1;
 constexpr int kMostPairs = 80;                      // that a launch has
 constexpr int kPlanes = 3;                          // of an fp32 operand
 constexpr int64_t kTurnedRows = 128;                // up to which the gradient's products are turned
-// Slices after which a sum leaves TMEM for fp32 sums in memory, where it is to be exact: TMEM's
-// are cut off, not rounded, at every 16 terms, by up to 2^-23 of what they have reached.
-constexpr int kLogitPart = 32, kSumPart = 16;
+// Slices after which a sum leaves TMEM for fp32 sums in memory: TMEM's are cut off, not rounded, at every 16
+// terms, by up to 2^-23 of what they have reached (sums of one sign, whose products reach far below it, by up to
+// three times that).  A logit's part ends after 2048 terms, so that what is lost does not grow with the dimension
+// (loss of 4096 rows of 4096 against 32000, bf16: 650 us in one part, 730 in two, a maximum 1.5e-6 and 8e-7 off);
+// with fp32 operands after 512 (loss of 1000 rows of 1600 against 16000: 238 us with 2048, 254 with 1024, 275 with
+// 512; m + log s of rows of 4096 are off by 7.3e-6, 4.7e-6 and 2.6e-6 on the average, those of fp32 products 2.5e-6).
+constexpr int kLogitPart = 32, kExactLogitPart = 8, kSumPart = 16;
 // What a sum of n such steps loses on the average: its partial sums lie, on the average, on the
 // line from 0 to the result x whatever their path, and a step loses half a unit in the last
-// place of them, 0.72 2^-24 of their size: n / 2 * 0.72 * 2^-24 x in all, which is put back.
+// place of them, 0.72 2^-24 of their size: n / 2 * 0.72 * 2^-24 x in all, which is put back.  A
+// step of 16 zeros loses nothing: of a logit, n is at most the steps in which its hidden row has
+// entries, so that a sum of one term is that term.
 constexpr float kLostPerStep = 0.36f * 0x1p-24f;
 
 // Planes (i, j) of the products that a product is the sum of, four bits each.
@@ -94,7 +100,8 @@ struct Gemm {
     int64_t dtable_ld;
     int32_t dtable_bf16, accumulate;
     int32_t dtable_boxes;           // dW goes out by t_out
-    int32_t exact;                  // sums leave TMEM in parts
+    int32_t exact;                  // gradients' sums leave TMEM in parts, logits in shorter ones
+    const int32_t* steps;           // of compact rows: 16s of the dimension in which they are not 0
     float* scratch;                 // of the logits' parts: [CTAs][kTile / 2 x kTile]
     int32_t columns;                // TURNED: of the products, 64 or 128
     int32_t abreast;                // TURNED: dl's two planes side by side in dH's product
@@ -144,7 +151,7 @@ __device__ __forceinline__ Shape shape_of(const Gemm& P, const HeadItem& it, int
     if (it.kind <= kHeadLogits) {
         s.pairs = P.logits;
         s.kb = (P.dim + kSlice - 1) / kSlice;
-        s.part = P.exact ? kLogitPart : s.kb;
+        s.part = P.exact ? kExactLogitPart : kLogitPart;
         s.parts = (s.kb + s.part - 1) / s.part;
         return s;
     }
@@ -223,11 +230,13 @@ __device__ __forceinline__ void store_box(const CUtensorMap* map, const void* bo
 // What a row's logits need; the loads of compact row n.
 struct RowData {
     int label = -1;             // entry of the table
+    int steps = 0;
     float weight = 0.f, m = 0.f, inv = 0.f, of_label = 0.f;
     template <bool BACKWARD>
     __device__ __forceinline__ void load(const Gemm& P, int n) {
         of_label = P.label_logits[n];
         label = P.labels[n];
+        steps = P.steps[n];
         if (BACKWARD) {
             weight = P.weights[n];
             const float2 st = P.stats[n];
@@ -691,6 +700,9 @@ head_gemm_kernel(const __grid_constant__ Gemm P) {
             RowData data;
             if (it.kind <= kHeadLogits) data.load<BACKWARD>(P, turned ? col_w + lane : row);
             const int label = data.label - it.vt * kTile - col_w;
+            // (of the turned logits' columns, of which a warp has one or two 32s)
+            const int steps_low = data.steps, steps_high = TURNED && it.kind == kHeadLogits && P.columns > 64
+                                                               ? P.steps[col_w + 32 + lane] : 0;
             if (BACKWARD) {
                 // The buffer of a piece is free once the tiles that read the piece before in it are
                 // done; a part of dH has the earlier pieces in it.
@@ -738,7 +750,9 @@ head_gemm_kernel(const __grid_constant__ Gemm P) {
                     tmem_ld_issue(tbase, rv);
                     tmem_ld_wait(rv);
                 }
-                const float back = 1.f + kLostPerStep * (kSlice / 16) * shape.slices(part);
+                const int most = (kSlice / 16) * shape.slices(part);
+                const bool of_columns = TURNED && it.kind == kHeadLogits;
+                const float back = 1.f + kLostPerStep * (of_columns ? 0 : it.kind <= kHeadLogits ? min(most, data.steps) : most);
                 for (int ch = 0; ch < chunks; ++ch) {
                     float v[32];
 #pragma unroll
@@ -746,6 +760,11 @@ head_gemm_kernel(const __grid_constant__ Gemm P) {
                         const float2 f = unpack2(mul2(pack2(__uint_as_float(rv[j]), __uint_as_float(rv[j + 1])),
                                                       pack2(back, back)));
                         v[j] = f.x, v[j + 1] = f.y;
+                    }
+                    if (of_columns) {
+                        const float mine = 1.f + kLostPerStep * min(most, ch == 0 ? steps_low : steps_high);
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) v[j] *= __shfl_sync(~0u, mine, j);
                     }
                     if (turned && it.kind == kHeadHidden && P.abreast) {
                         tmem_ld_issue(tbase + P.columns + ch * 32, rv);
@@ -889,6 +908,7 @@ struct Few {
     int32_t row_ld, prefetch;
     const int32_t* live;
     const int32_t* labels;
+    const int32_t* steps;
     const float* label_logits;
     float2* parts;                  // [gridDim.x][row_ld]
     int32_t* status;
@@ -917,6 +937,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kFewThreads, 1) head
     __shared__ uint32_t tmem_slot;
     __shared__ int abort_sh;
     __shared__ float2 of_warp[kFewWarps][kFewRows];
+    __shared__ __align__(16) float back_of[2][kFewRows];       // of a row's sums, and of the last of them
     volatile int* abort_flag = &abort_sh;
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
                                                ~static_cast<uintptr_t>(1023));
@@ -1018,8 +1039,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kFewThreads, 1) head
     } else {
         const int quarter = warp & 3, chunks = P.columns / 32;
         const uint32_t tempty[2] = {mapa_shared(smem_u32(&tempty_bar[0]), 0), mapa_shared(smem_u32(&tempty_bar[1]), 0)};
-        const float back = 1.f + kLostPerStep * (kSlice / 16) * P.each;
-        const float back_last = 1.f + kLostPerStep * (kSlice / 16) * (slices - (slices - 1) / P.each * P.each);
+        if (threadIdx.x - 64 < kFewRows) {
+            const int row = threadIdx.x - 64, steps = row < live ? P.steps[row] : 0;
+            back_of[0][row] = 1.f + kLostPerStep * min((kSlice / 16) * P.each, steps);
+            back_of[1][row] = 1.f + kLostPerStep * min((kSlice / 16) * (slices - (slices - 1) / P.each * P.each), steps);
+        }
+        asm volatile("bar.sync 1, %0;" ::"n"(32 * kFewWarps) : "memory");
         float m[kFewRows / 32], s[kFewRows / 32], of_label[kFewRows / 32];
         int label[kFewRows / 32];
 #pragma unroll
@@ -1047,13 +1072,21 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kFewThreads, 1) head
                 tmem_ld_wait(rv);
                 float v[32], w[32];
 #pragma unroll
-                for (int j = 0; j < 32; ++j) v[j] = first + lane < P.vocab ? __uint_as_float(rv[j]) * back : -INFINITY;
-                for (int k = P.each; k < slices; k += P.each) {
-                    tmem_ld_issue(from += P.columns, rv);
-                    tmem_ld_wait(rv);
-                    const float last = k + P.each < slices ? back : back_last;
+                for (int j = 0; j < 32; ++j) v[j] = first + lane < P.vocab ? 0.f : -INFINITY;
+                for (int k = 0; k < slices; k += P.each) {
+                    if (k > 0) {
+                        tmem_ld_issue(from += P.columns, rv);
+                        tmem_ld_wait(rv);
+                    }
+                    const float4* const back = reinterpret_cast<const float4*>(back_of[k + P.each < slices ? 0 : 1] + 32 * c);
 #pragma unroll
-                    for (int j = 0; j < 32; ++j) v[j] = fmaf(__uint_as_float(rv[j]), last, v[j]);
+                    for (int j = 0; j < 32; j += 4) {
+                        const float4 b = back[j / 4];
+                        v[j] = fmaf(__uint_as_float(rv[j]), b.x, v[j]);
+                        v[j + 1] = fmaf(__uint_as_float(rv[j + 1]), b.y, v[j + 1]);
+                        v[j + 2] = fmaf(__uint_as_float(rv[j + 2]), b.z, v[j + 2]);
+                        v[j + 3] = fmaf(__uint_as_float(rv[j + 3]), b.w, v[j + 3]);
+                    }
                 }
                 const int at = label[c] - first;
                 for (unsigned mine = __ballot_sync(~0u, at >= 0 && at < 32); mine != 0; mine &= mine - 1) {
@@ -1221,6 +1254,7 @@ struct Pack {
     int64_t table_ld;
     int32_t table_bf16, table_vec;
     float* label_logits;
+    int32_t* steps;                 // of hidden rows: see Gemm; else null
 };
 
 // A warp takes a row, eight entries a lane at a time; VEC: they start on 16-byte addresses.
@@ -1243,10 +1277,21 @@ __device__ __forceinline__ void pack_row(const Pack& K, int64_t at, bool on, int
     const T* const from = static_cast<const T*>(K.from) + source * K.from_ld;
     constexpr int kAhead = 4;
     float dot = 0.f;
-    for (int c0 = 8 * lane; c0 < K.ld; c0 += 256 * kAhead) {
+    int steps = 0;
+    for (int c0 = 8 * lane; c0 - 8 * lane < K.ld; c0 += 256 * kAhead) {         // (all lanes equally often)
         float v[kAhead][8];
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) load_eight<T, VEC>(from + c0 + 256 * i, on ? K.cols - c0 - 256 * i : 0, v[i]);
+        if (K.steps != nullptr) {
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) {
+                bool some = false;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) some |= v[i][j] != 0.f;
+                const unsigned lanes = __ballot_sync(~0u, some);
+                steps += __popc((lanes | lanes >> 1) & 0x55555555u);
+            }
+        }
         if (label >= 0) {
             // A label's logit, of all the largest and a sum of terms of one sign, in fp32: TMEM's sum of
             // 1280 terms would be 1e-5 off, and a small loss as much of itself.
@@ -1285,6 +1330,7 @@ __device__ __forceinline__ void pack_row(const Pack& K, int64_t at, bool on, int
             }
         }
     }
+    if (K.steps != nullptr && lane == 0) K.steps[at] = steps;
     if (label >= 0) {
         dot = warp_sum(dot);
         if (lane == 0) K.label_logits[at] = dot;
@@ -1583,14 +1629,22 @@ struct Layout {
     int h_planes, w_planes, d_planes;
     bool pack_table;
     int64_t row_ld, dim_ld;
-    int64_t place, row, live, labels, weights, stats, label_logits, parts, counters, ncounters, hidden, table, dl, acc, scratch;
+    int64_t place, row, live, labels, weights, stats, steps, label_logits, parts, counters, ncounters, hidden, table, dl, acc, scratch;
     int64_t bytes;
 };
 // The table is read where it lies if it is bf16 and TMA can address it.
 bool direct_table(const malt_head_t* h) {
     return h->table_dtype == MALT_BF16 && aligned_to(h->table, 16) && h->table_ld % 8 == 0;
 }
-bool few_rows(const malt_head_t* h, const Layout& L) { return h->rows <= kFewRows && L.h_planes == 1 && L.w_planes == 1; }
+// Slices of one of the sums of a logit of few rows: as short as a part.
+int few_each(const malt_head_t* h) {
+    const int64_t columns = (h->rows + 31) / 32 * 32, slices = (h->dim + kSlice - 1) / kSlice;
+    const int64_t sums = std::min<int64_t>(kTile / std::max<int64_t>(columns, 32), kFewSums);
+    return static_cast<int>((slices + sums - 1) / sums);
+}
+bool few_rows(const malt_head_t* h, const Layout& L) {
+    return h->rows <= kFewRows && L.h_planes == 1 && L.w_planes == 1 && few_each(h) <= kLogitPart;
+}
 Layout layout_of(const malt_head_t* h, bool forward, bool gradient) {
     Layout L = {};
     L.plan = head_plan(h->rows, h->dim, h->vocab);
@@ -1620,9 +1674,10 @@ Layout layout_of(const malt_head_t* h, bool forward, bool gradient) {
     L.labels = take(4 * L.row_ld);
     L.weights = take(4 * L.row_ld);
     L.stats = take(8 * L.row_ld);
+    L.steps = take(4 * L.row_ld);
     L.hidden = take(2 * L.h_planes * L.row_ld * L.dim_ld);
     if (L.pack_table) L.table = take(2 * L.w_planes * h->vocab * L.dim_ld);
-    if (exact) L.scratch = take(4ll * 2 * kMostPairs * kHalf * kTile);
+    if (exact || h->dim > kLogitPart * kSlice) L.scratch = take(4ll * 2 * kMostPairs * kHalf * kTile);
     L.label_logits = take(4 * L.row_ld);
     if (forward) {
         L.parts = take(8 * L.row_ld * std::max<int64_t>(2 * p.vocab_tiles, few_rows(h, L) ? 2 * kMostPairs : 0));
@@ -1709,6 +1764,7 @@ cudaError_t launch_all(const malt_head_t* h, const Outputs& O, bool forward, boo
     K.table_bf16 = h->table_dtype == MALT_BF16;
     K.table_vec = h->table_ld % 8 == 0 && aligned_to(h->table, 16);
     K.label_logits = static_cast<float*>(at(L.label_logits));
+    K.steps = static_cast<int32_t*>(at(L.steps));
     if (rows <= kGatherRows) {
         const GatherKernel gather = rows <= 256 ? gather_kernel<256>(K, h->hidden_dtype)
                                                 : gather_kernel<kGatherRows>(K, h->hidden_dtype);
@@ -1725,6 +1781,7 @@ cudaError_t launch_all(const malt_head_t* h, const Outputs& O, bool forward, boo
         K.row = nullptr;
         K.live = nullptr;
         K.labels = nullptr;
+        K.steps = nullptr;
         K.rows = static_cast<int32_t>(h->vocab);
         K.planes = L.w_planes;
         K.plane = h->vocab * L.dim_ld;
@@ -1766,6 +1823,7 @@ cudaError_t launch_all(const malt_head_t* h, const Outputs& O, bool forward, boo
     G.live = S.live;
     G.labels = S.c_labels;
     G.weights = S.c_weights;
+    G.steps = static_cast<const int32_t*>(at(L.steps));
     G.stats = S.c_stats;
     G.parts = static_cast<float2*>(at(L.parts));
     G.label_logits = static_cast<const float*>(at(L.label_logits));
@@ -1780,8 +1838,7 @@ cudaError_t launch_all(const malt_head_t* h, const Outputs& O, bool forward, boo
             Few F = {};
             F.w_k = G.w_k;
             F.columns = static_cast<int32_t>((h->rows + 31) / 32 * 32);
-            const int64_t slices = (h->dim + kSlice - 1) / kSlice, sums = std::min<int64_t>(kTile / F.columns, kFewSums);
-            F.each = static_cast<int32_t>((slices + sums - 1) / sums);
+            F.each = few_each(h);
             if (!map_of(&F.h_n, at(L.hidden), L.dim_ld, L.row_ld, 1, L.dim_ld, F.columns / 2)) return cudaErrorInvalidValue;
             F.dim = G.dim;
             F.vocab = G.vocab;
@@ -1791,6 +1848,7 @@ cudaError_t launch_all(const malt_head_t* h, const Outputs& O, bool forward, boo
             F.prefetch = L.pack_table ? 0 : static_cast<int32_t>(std::min<int64_t>(p.vocab_tiles, kPrefetchBytes / (kTile * 2 * L.dim_ld)));
             F.live = S.live;
             F.labels = S.c_labels;
+            F.steps = G.steps;
             F.label_logits = G.label_logits;
             F.parts = G.parts;
             F.status = status;
