@@ -109,3 +109,23 @@ def test_long_sums_of_one_sign(rows, dim, filled):
     want = (X.double() @ W.double().t()).max(1).values
     off = stats[:, 0].double() / want - 1
     assert abs(float(off.mean())) < 7e-7, float(off.mean())
+
+
+@pytest.mark.parametrize("rows,dim,vocab", [(300, 739, 964), (300, 1600, 3000), (300, 4096, 2000)])
+def test_gradients_on_statistics_from_elsewhere(rows, dim, vocab):
+    """The gradient is that of the given statistics, here those of torch's fp32 products, to what logits of our own
+    are off by: parts of 512 terms, of which each loses about two ulp of a partial sum of some units (2.4e-7 each)
+    beside what is put back, eight of them 1.4e-6; a row's dl is as much of itself off, of which 2e-6 is the bound."""
+    torch, ops = torch_and_ops()
+    g = torch.Generator(device="cuda").manual_seed(dim)
+    W = torch.randn(vocab, dim, generator=g, device="cuda") * 0.05
+    Y = torch.randint(0, vocab, (rows,), generator=g, device="cuda")
+    X = torch.randn(rows, dim, generator=g, device="cuda") + W[Y] * (8.0 / (0.0025 * dim))
+    x = X @ W.t()
+    m = x.amax(1)
+    stats = torch.stack([m, (x - m[:, None]).exp().sum(1)], 1)
+    dh, dw = ops.head_grad(X, W, Y, stats)
+    p = torch.exp(X.double() @ W.double().t() - stats[:, :1].double()) / stats[:, 1:].double()
+    p[torch.arange(rows, device="cuda"), Y] -= 1
+    for got, want in ((dh, p @ W.double()), (dw, p.t() @ X.double())):
+        assert float((got.double() - want).norm() / want.norm()) < 2e-6
