@@ -807,8 +807,9 @@ class AdamW8:
     def __init__(self, params, seed: int = 0, stream=None):
         import torch
         self.params = tuple(map(tuple, params))
-        self._tensors = [t for p in self.params for t in p if isinstance(t, torch.Tensor)]
+        self._tensors = [t for p in self.params for t in p[:7] if t is not None]
         self._codes = [t for p in self.params for t in p[3:7]]
+        self._address, self._current_stream = torch.Tensor.data_ptr, torch._C._cuda_getCurrentRawStream
         self._array = adamw8_params_array(self.params)
         self._at, self._codes_at = self._addresses(self._tensors), self._addresses(self._codes)
         self._elements = sum(-(-p[0].numel() // ADAMW8_BLOCK) for p in self.params) * ADAMW8_BLOCK
@@ -816,10 +817,8 @@ class AdamW8:
         self._on = torch.device("cuda", self._device)
         self.state = _adamw8_init(self.params, self._array, seed, stream)
 
-    @staticmethod
-    def _addresses(tensors):
-        import torch
-        return list(map(torch.Tensor.data_ptr, tensors))
+    def _addresses(self, tensors):
+        return list(map(self._address, tensors))
 
     def _moved(self):
         """The tensors checked again, where they lie now."""
@@ -853,8 +852,7 @@ class AdamW8:
 
     def _stream(self, stream):
         """The raw handle of a stream, by default the current one of the tensors' device."""
-        import torch
-        return stream.cuda_stream if stream is not None else torch._C._cuda_getCurrentRawStream(self._device)
+        return stream.cuda_stream if stream is not None else self._current_stream(self._device)
 
     def spans(self):
         """(first, end) of each tensor's elements in what moments returns."""

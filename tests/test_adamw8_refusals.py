@@ -26,6 +26,7 @@ def test_tensors_on_another_device(monkeypatch):
             with pytest.raises(ValueError, match="current CUDA device"):
                 make()
     opt = malt.AdamW8.__new__(malt.AdamW8)
+    opt._address = torch.Tensor.data_ptr
     opt.state, opt.params, opt._device, opt._on = None, (entry(),), 0, torch.device("cuda", 0)
     with pytest.raises(ValueError, match="where the state is"):
         opt.step(malt.adamw_hparams(), params=[entry()])
