@@ -416,6 +416,8 @@ head_gemm_kernel(const __grid_constant__ Gemm P) {
     __shared__ __align__(8) uint64_t full_bar[kRing], empty_bar[kRing], tfull_bar[2], tempty_bar[2], drain_bar;
     __shared__ __align__(8) uint64_t item_full[kItemSlots], item_empty[kItemSlots], sig_bar[kSigSlots];
     __shared__ __align__(16) int4 item_ring[kItemSlots];
+    // TURNED: what puts back the loss of a logit's part, and of its last one, per compact row
+    __shared__ __align__(16) float back_of[TURNED ? 2 : 1][TURNED ? kTurnedRows : 4];
     __shared__ uint32_t tmem_slot;
     __shared__ int abort_sh;
     volatile int* abort_flag = &abort_sh;
@@ -677,6 +679,14 @@ head_gemm_kernel(const __grid_constant__ Gemm P) {
         const int ew = warp - 2, quarter = warp & 3;
         const uint32_t tempty[2] = {mapa_shared(smem_u32(&tempty_bar[0]), 0), mapa_shared(smem_u32(&tempty_bar[1]), 0)};
         int obuf = 0, turn = 0;
+        if constexpr (TURNED) {
+            static_assert(32 * kEpiWarps == 2 * kTurnedRows, "a thread has a row's factor of one kind");
+            const int n = 32 * ew + lane, of_row = n % kTurnedRows, slices = (P.dim + kSlice - 1) / kSlice;
+            const int whole = P.exact ? kExactLogitPart : kLogitPart, last = slices - (slices - 1) / whole * whole;
+            back_of[n / kTurnedRows][of_row] =
+                1.f + kLostPerStep * min((kSlice / 16) * (n < kTurnedRows ? whole : last), P.steps[of_row]);
+            asm volatile("bar.sync 1, %0;" ::"n"(32 * kEpiWarps) : "memory");
+        }
         for (int seq = 0;; ++seq) {
             int index = kEnd, ok = 1;
             if (lane == 0) ok = ring_item(seq, index) ? 1 : 0;
@@ -700,9 +710,6 @@ head_gemm_kernel(const __grid_constant__ Gemm P) {
             RowData data;
             if (it.kind <= kHeadLogits) data.load<BACKWARD>(P, turned ? col_w + lane : row);
             const int label = data.label - it.vt * kTile - col_w;
-            // (of the turned logits' columns, of which a warp has one or two 32s)
-            const int steps_low = data.steps, steps_high = TURNED && it.kind == kHeadLogits && P.columns > 64
-                                                               ? P.steps[col_w + 32 + lane] : 0;
             if (BACKWARD) {
                 // The buffer of a piece is free once the tiles that read the piece before in it are
                 // done; a part of dH has the earlier pieces in it.
@@ -752,19 +759,24 @@ head_gemm_kernel(const __grid_constant__ Gemm P) {
                 }
                 const int most = (kSlice / 16) * shape.slices(part);
                 const bool of_columns = TURNED && it.kind == kHeadLogits;
-                const float back = 1.f + kLostPerStep * (of_columns ? 0 : it.kind <= kHeadLogits ? min(most, data.steps) : most);
+                const float back = 1.f + kLostPerStep * (it.kind <= kHeadLogits ? min(most, data.steps) : most);
                 for (int ch = 0; ch < chunks; ++ch) {
                     float v[32];
-#pragma unroll
-                    for (int j = 0; j < 32; j += 2) {
-                        const float2 f = unpack2(mul2(pack2(__uint_as_float(rv[j]), __uint_as_float(rv[j + 1])),
-                                                      pack2(back, back)));
-                        v[j] = f.x, v[j + 1] = f.y;
-                    }
                     if (of_columns) {
-                        const float mine = 1.f + kLostPerStep * min(most, ch == 0 ? steps_low : steps_high);
+                        const float4* const of_row = reinterpret_cast<const float4*>(back_of[TURNED && part + 1 == parts] + col_w + ch * 32);
 #pragma unroll
-                        for (int j = 0; j < 32; ++j) v[j] *= __shfl_sync(~0u, mine, j);
+                        for (int j = 0; j < 32; j += 4) {
+                            const float4 b = of_row[j / 4];
+                            v[j] = __uint_as_float(rv[j]) * b.x, v[j + 1] = __uint_as_float(rv[j + 1]) * b.y;
+                            v[j + 2] = __uint_as_float(rv[j + 2]) * b.z, v[j + 3] = __uint_as_float(rv[j + 3]) * b.w;
+                        }
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < 32; j += 2) {
+                            const float2 f = unpack2(mul2(pack2(__uint_as_float(rv[j]), __uint_as_float(rv[j + 1])),
+                                                          pack2(back, back)));
+                            v[j] = f.x, v[j + 1] = f.y;
+                        }
                     }
                     if (turned && it.kind == kHeadHidden && P.abreast) {
                         tmem_ld_issue(tbase + P.columns + ch * 32, rv);
