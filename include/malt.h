@@ -698,8 +698,8 @@ int malt_distill_forward_backward(const malt_distill_t* d, float* loss, float* s
  * alignments, 0 for what the calls refuse.  Workspaces are 256-byte aligned.
  * Outputs and workspace may not lie in the inputs' memory or in one another's
  * (columns of one matrix apart do not).  Should a wait
- * inside a kernel run out (a second and more: nothing here waits that long), all
- * losses and dhidden are NaN, and dtable is not to be used.
+ * inside a kernel run out (a second and more: nothing here waits that long), dhidden
+ * is NaN, dtable is not to be used, and losses are NaN if it was in the forward pass.
  * rows <= 2^22, dim <= 2^16, vocab <= 2^24, and fewer than 2^30 tiles of 256. */
 typedef struct {
     const void*  hidden;        /* rows x dim                                 */

@@ -338,7 +338,8 @@ def rms_norm(x, gain, residual=None, eps: float = 1e-6, dtype=None, out=None, re
     """(y, h): h = x + residual, rounded to the residual's type (x itself without one), and every row
     of h divided by its root mean square and multiplied by gain (None: ones), in `dtype` (default:
     x's).  out (y) and residual_out (h) may be given, each also as x or the residual
-    (its type and layout), not both as one."""
+    (its type and layout), not both as one, and else apart from them (with out=x and no
+    residual x is y, and no h is left for the gradient)."""
     if stream is not None:
         return _on(stream, rms_norm, x, gain, residual, eps, dtype, out, residual_out)
     dev = _device("x gain residual out residual_out", x, gain, residual, out, residual_out)
