@@ -25,7 +25,7 @@
 //
 // Bound by the tensor cores: 2 N V D flop forward, 8 N V D with the gradients (6 with the
 // logits kept), and for few rows by reading the table.  8192 rows of 1280 against 50304, a tenth
-// left out: 2.39 to 2.55 ms for loss and gradients, 1.49 to 1.59 PFLOP/s at the power cap
+// left out: 2.39 to 2.72 ms for loss and gradients, 1.40 to 1.59 PFLOP/s at the power cap
 // (the forward product alone 495 us, 1.94 PFLOP/s).
 #include <cuda.h>
 #include <cudaTypedefs.h>
