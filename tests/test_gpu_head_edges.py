@@ -1,9 +1,11 @@
-"""The output head at its edges: operands in one matrix, sums in parts, views of a table whose rows are no whole
-16 bytes."""
+"""The output head at its edges: operands in one matrix, sums in parts, rows of few entries, views of a table whose
+rows are no whole 16 bytes."""
+import numpy as np
 import pytest
 
-from tests.test_gpu_head import BF16, case
-from tests.test_gpu_model_ops import placed, torch_and_ops
+from oracle import model_ops_ref as ref
+from tests.test_gpu_head import BF16, F32, bounds, case
+from tests.test_gpu_model_ops import U, check, out_bound, placed, torch_and_ops
 
 pytestmark = pytest.mark.gpu
 
@@ -60,6 +62,32 @@ def test_fp32_sums_in_parts(rows, dim, vocab, accumulate):
     assert near(dw.double() - old if accumulate else dw, want, 5e-6)
 
 
+@pytest.mark.parametrize("rows,dim,vocab", [(24, 2200, 300), (128, 4099, 520), (300, 2200, 600), (520, 4160, 700)])
+@pytest.mark.parametrize("table_type", [BF16, F32])
+def test_bf16_logits_in_parts(rows, dim, vocab, table_type):
+    """Loss and gradients of bf16 rows longer than a part; element by element, within the bounds of their sums."""
+    torch, ops = torch_and_ops()
+    exact = table_type == F32
+    hidden, table, labels, weight = case(rows, dim, vocab, BF16, table_type, seed=dim)
+    X, W = torch.as_tensor(hidden).bfloat16().cuda(), torch.as_tensor(table).to(getattr(torch, table_type)).cuda()
+    Y, C = torch.as_tensor(labels).cuda(), torch.as_tensor(weight).cuda()
+    loss, m, s, dhidden, dtable = ref.head(hidden, table, labels, weight)
+    b_loss, b_m, b_s, b_dh, b_dt = bounds(hidden, table, labels, weight, np.ones(rows), exact)
+    got, stats = ops.head_loss(X, W, Y, weight=C)
+    check(got, loss, b_loss, "loss")
+    check(stats[:, 0], m, b_m + U * np.abs(m), "m")
+    check(stats[:, 1], s, s * (b_s + b_m), "s")
+    both, dh, dw = ops.head_loss_grad(X, W, Y, weight=C, dtype=torch.float32)
+    assert torch.equal(both, got)
+    check(dh, dhidden, out_bound(dhidden, b_dh, dh.dtype), "dhidden")
+    check(dw, dtable, out_bound(dtable, b_dt, dw.dtype), "dtable")
+    dh2, dw2 = ops.head_grad(X, W, Y, stats, weight=C, dtype=torch.float32)
+    assert torch.equal(dh2, dh) and torch.equal(dw2, dw)
+    # far below the bounds: dl's and the result's rounding
+    near = lambda a, b, tol: float(np.linalg.norm(a.double().cpu().numpy() - b) / np.linalg.norm(b)) < tol
+    assert near(got, loss, 1e-5) and near(dh, dhidden, 2.0 ** -8) and near(dw, dtable, 5e-6 if exact else 2.0 ** -8)
+
+
 def test_views_of_a_table_with_odd_rows():
     """Rows whose last 16 bytes are shared with what lies behind them: it is not read into the logits."""
     torch, ops = torch_and_ops()
@@ -91,7 +119,7 @@ def test_rows_of_one_entry(rows, dim):
 
 
 @pytest.mark.parametrize("rows", [24, 100, 300])
-@pytest.mark.parametrize("dim,filled", [(1280, 1280), (1600, 800), (4096, 4096), (4096, 2048)])
+@pytest.mark.parametrize("dim,filled", [(1280, 1280), (1600, 800), (4096, 4096), (4096, 2048), (8200, 8200)])
 def test_long_sums_of_one_sign(rows, dim, filled):
     """What a tensor core's cut-off sums lose on the average is put back, for as many terms as there are.
 
