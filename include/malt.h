@@ -481,8 +481,9 @@ void malt_adamw8_destroy_state(malt_adamw8_state_t* st);
  * elements, in two device buffers of dtype MALT_F32 or MALT_BF16 (both exact).
  * get writes zeros behind a tensor's elements; set rounds to the nearest code
  * (a negative s makes both NaN, -0 is 0).  Enqueued on `stream`, one of them at a
- * time; get changes nothing that a step reads, and one that runs beside a step
- * takes old or new codes.  get_step waits for the last step's stream alone. */
+ * time, set in the caller's order with the steps.  get changes nothing that a step
+ * reads; beside a step it may find codes and exponents of before and after it.
+ * get_step and set_step synchronise with the last step's stream. */
 int malt_adamw8_get_moments(malt_adamw8_state_t* st, const malt_adamw8_param_t* params, int32_t n, void* m, void* root,
                             int32_t dtype, void* stream);
 int malt_adamw8_set_moments(malt_adamw8_state_t* st, const malt_adamw8_param_t* params, int32_t n, const void* m,
@@ -607,8 +608,8 @@ int malt_qk_norm_backward(const malt_qk_norm_t* p, const malt_heads_t* dq_out, c
  * call refuses; without dgain none is needed).
  * h and y may each be x's or the residual's buffer (not both the same), dx dy's,
  * h's or dh's, with the same leading dimension and type; else what is written may
- * not lie in another operand's memory.  dim and leading dimensions
- * that are multiples of 8 on 16-byte addresses (codes 8) run faster.  dim <= 2^24,
+ * not lie in another operand's memory.  dim and leading dimensions that are
+ * multiples of 8 on 16-byte addresses (codes 8) run faster.  dim <= 2^24,
  * tokens < 2^31 - 64. */
 typedef struct {
     const void* gain;           /* dim entries, or NULL for ones              */
@@ -697,9 +698,9 @@ int malt_distill_forward_backward(const malt_distill_t* d, float* loss, float* s
  * the calls (forward, gradient: which of them) on these sizes, types and
  * alignments, 0 for what the calls refuse.  Workspaces are 256-byte aligned.
  * Outputs and workspace may not lie in the inputs' memory or in one another's
- * (columns of one matrix apart do not).  Should a wait
- * inside a kernel run out (a second and more: nothing here waits that long), dhidden
- * is NaN, dtable is not to be used, and losses are NaN if it was in the forward pass.
+ * (columns of one matrix apart do not).  Should a wait inside a kernel run out (a
+ * second and more: nothing here waits that long), dhidden is NaN, dtable is not to
+ * be used, and losses are NaN if it was in the forward pass.
  * rows <= 2^22, dim <= 2^16, vocab <= 2^24, and fewer than 2^30 tiles of 256. */
 typedef struct {
     const void*  hidden;        /* rows x dim                                 */

@@ -267,8 +267,9 @@ __device__ __forceinline__ uint32_t signed_codes(uint32_t a, uint32_t b, uint32_
 // Whether a byte is 0xff.
 __device__ __forceinline__ bool has_nan(uint32_t u) { return (((u & 0x7f7f7f7fu) + 0x01010101u) & u & 0x80808080u) != 0; }
 
-// The same in pairs: the same weights, moments' values and exponents (a negative m that rounds to zero has
-// code 0x80 here, 0 there); the quotient that w takes is an approximate one, within 2 ulp.  The instructions per entry decide the kernel's time (66 M entries: 288 us with 106 of
+// The same in pairs: the same weights, moments' values and exponents (a negative m that rounds
+// to zero has code 0x80 here, 0 there); the quotient that w takes is an approximate one, within
+// 2 ulp.  The instructions per entry decide the kernel's time (66 M entries: 288 us with 106 of
 // them, 179 with 69 and operands copied ahead).
 __device__ __forceinline__ void update(Entries& x, const Hyper& h, float step, float root_scale, float decay,
                                        uint32_t first, uint32_t key) {

@@ -800,9 +800,9 @@ class AdamW8:
     m_scale, v, v_scale, weight_decay) device tensors; the states (adamw8_states makes them) are zeroed at
     construction.  seed: of the states' random rounding.
 
-    The tensors are checked in full here, and again where one of them has moved (its `.data` was replaced, its
-    storage resized): checks of hundreds of tensors take the host longer than the GPU their update, a look at
-    their addresses half of it."""
+    The tensors are checked in full here, and again where one of them has another address (its `.data` was
+    replaced, its storage resized); one that stays where it is keeps its size and type.  Checks of hundreds of
+    tensors take the host longer than the GPU their update, a look at their addresses half of it."""
 
     def __init__(self, params, seed: int = 0, stream=None):
         import torch
